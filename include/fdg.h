@@ -298,6 +298,77 @@ FDG_API fdg_status fdg_bias_grad_static(const void* dev_dy, int32_t dtype, int64
                                         float* dev_db, void* stream);
 FDG_API const char* fdg_static_last_error(void);
 
+/* Operators on token sequences, on the caller's tensors and stream: what a network of FDG_EMBEDDING and FDG_RECURRENCE layers and a
+ * distillation loss computes inside fdg_step, for callers that run their own loop (or serve a trained network).
+ *
+ * Conventions of all of them
+ *   - Pointers are device memory of the CURRENT device (checked; FDG_ERR_INVALID_ARG otherwise), on their elements' natural alignment, and cover the
+ *     sizes and strides given (not checked).  dtype 0: fp32, 1: bf16.  Strides are in elements.  Outputs overlap neither inputs nor each other
+ *     unless it says so.  Any size works; rows that start on 16 bytes (pointers and strides) are the fast ones.
+ *   - A call only enqueues kernels on `stream` (a cudaStream_t, NULL: the default stream): no allocation, no synchronisation, nothing kept between
+ *     calls, so it may be captured into a CUDA graph, and calls on different streams, with workspaces of their own, may overlap.
+ *   - Arithmetic and sums are in 32 bits, results are rounded once; equal inputs on equal devices give equal bits.
+ *   - A refused call launches nothing; fdg_op_last_error() says why (per thread). */
+
+/* Embedding lookup (the first layer of a token model): out[i] = scale * table[tokens[i]] for i < n.
+ *   tokens : int32 [n]; an id outside 0..vocab-1 (padding) gives a row of zeros
+ *   table  : [vocab][channels]
+ *   out    : n rows of `channels`, out_stride apart */
+FDG_API fdg_status fdg_embedding_forward(const int32_t* dev_tokens, int64_t n, const void* dev_table, int32_t dtype, int64_t vocab, int64_t channels, float scale,
+                                         void* dev_out, int64_t out_stride, void* stream);
+/* The table's gradient: dtable[v] = scale * sum over i with tokens[i] == v of dy[i]  (fp32; every row is written), or, accumulate != 0, that added to what
+ * dtable holds (rows that no token names are not touched).  Ids outside the table take no part, whatever their dy holds.
+ *   dy        : dtype, n rows of `channels`, dy_stride apart
+ *   workspace : fdg_embedding_workspace bytes, 256-byte aligned, the call's own until its kernels have run; nothing in it is read before it is written */
+FDG_API fdg_status fdg_embedding_workspace(int64_t n, int64_t vocab, int64_t channels, size_t* bytes);
+FDG_API fdg_status fdg_embedding_backward(const int32_t* dev_tokens, int64_t n, const void* dev_dy, int32_t dtype, int64_t dy_stride, int64_t vocab, int64_t channels,
+                                          float scale, int32_t accumulate, float* dev_dtable, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* Gated linear recurrence along the steps of `batch` sequences, every channel by itself:
+ *   a_t = sigmoid(gate_t),   h_t = a_t h_{t-1} + (1 - a_t) value_t,   y_t = h_t   (h_0 = state_in, or zero)
+ * A single step (steps = 1, state_in, state_out) serves one new token; state_out may be state_in.
+ * Tensors are [batch][steps][channels] with strides of their own between sequences and between steps, channels contiguous (so gate and value may be the
+ * halves of one tensor, or time-major).  state_*, dstate_* are fp32 [batch][channels], contiguous; saved is written by the forward call and read by the
+ * backward call of the same shape and dtype (fdg_recurrence_saved bytes, 16-byte aligned).
+ *   lengths : int32 [batch] or NULL.  Steps at or behind a sequence's length (clamped to 0..steps) do not count: y is zero there, the gradients are zero,
+ *             whatever gate, value and dy hold; state_out is h after the last step that counts.
+ * Backward: with d_t = dy_t + a_{t+1} d_{t+1} (and dstate_out added to the last), dvalue_t = (1 - a_t) d_t,
+ *   dgate_t = a_t (1 - a_t) d_t (h_{t-1} - value_t), dstate_in = a_1 d_1.  h is computed again in 32 bits from `saved`. */
+typedef struct {
+    int32_t dtype;
+    int64_t batch, steps, channels;
+    int64_t gate_batch, gate_step, value_batch, value_step;      /* strides of gate and value                 */
+    int64_t y_batch, y_step;                                     /* forward: of y                             */
+    int64_t dy_batch, dy_step;                                   /* backward: of dy                           */
+    int64_t dgate_batch, dgate_step, dvalue_batch, dvalue_step;  /* backward: of dgate and dvalue             */
+} fdg_recurrence;
+FDG_API fdg_status fdg_recurrence_saved(const fdg_recurrence* shape, size_t* bytes);
+FDG_API fdg_status fdg_recurrence_forward(const fdg_recurrence* shape, const void* dev_gate, const void* dev_value, const int32_t* dev_lengths_or_null,
+                                          const float* dev_state_in_or_null, void* dev_y, float* dev_state_out_or_null, void* dev_saved_or_null, void* stream);
+FDG_API fdg_status fdg_recurrence_backward(const fdg_recurrence* shape, const void* dev_gate, const void* dev_value, const int32_t* dev_lengths_or_null,
+                                           const void* dev_saved, const void* dev_dy, const float* dev_dstate_out_or_null, void* dev_dgate, void* dev_dvalue,
+                                           float* dev_dstate_in_or_null, void* stream);
+
+/* Loss that distils a teacher's top logits, with the gradient for the student's logits.  Per row, with p = softmax(teacher / temperature) over
+ * the row's `top` entries, q = softmax(logits / temperature) and q1 = softmax(logits) over the vocabulary, w = weight:
+ *   loss = w temperature^2 sum_j p_j (log p_j - log q[id_j]) + (1 - w) (-log q1[label])
+ *   dlogits_v = scale (w temperature (q_v - sum of the p_j with id_j == v) + (1 - w) (q1_v - [v == label]))
+ *   logits  : logits_dtype, rows of `vocab`, logits_stride apart
+ *   labels  : int32 [rows]; a label outside 0..vocab-1 takes its row out (loss and gradient zero).  NULL (weight 1 only): every row counts
+ *   ids, teacher : int32, fp32 [rows][top]; an entry whose id is outside the vocabulary is left out, as is one of logit -infinity; entries with the same
+ *             id count one by one; a row without an entry has no distillation term.  Not read when weight is 0 (may be NULL)
+ *   loss    : fp32 [rows]
+ *   dlogits : dlogits_dtype, or NULL for the loss alone; may be `logits` itself (same type and stride)
+ * Types: logits and dlogits of the same type, or fp32 logits and bf16 dlogits.  vocab <= 262144, top <= 1024, temperature > 0, 0 <= weight <= 1. */
+typedef struct {
+    int32_t logits_dtype, dlogits_dtype, top;
+    int64_t rows, vocab, logits_stride, dlogits_stride;
+    float temperature, weight, scale;
+} fdg_distill;
+FDG_API fdg_status fdg_distill_loss(const fdg_distill* d, const void* dev_logits, const int32_t* dev_labels_or_null, const int32_t* dev_ids, const float* dev_teacher,
+                                    float* dev_loss, void* dev_dlogits_or_null, void* stream);
+FDG_API const char* fdg_op_last_error(void);
+
 FDG_API const char* fdg_last_error(const fdg_ctx* ctx);   /* ctx may be NULL: last create error */
 FDG_API void        fdg_destroy(fdg_ctx* ctx);
 

@@ -23,6 +23,8 @@ EXPORTS = ["fdg_create", "fdg_grid_sms", "fdg_param_count", "fdg_param_layout", 
            "fdg_grads_worker", "fdg_consensus_error", "fdg_step", "fdg_step_host", "fdg_wait_ingest", "fdg_join", "fdg_params",
            "fdg_grads", "fdg_trace", "fdg_set_lr", "fdg_stats", "fdg_module_times", "fdg_profile", "fdg_profile_read",
            "fdg_bias_grad_static", "fdg_static_last_error",
+           "fdg_embedding_forward", "fdg_embedding_workspace", "fdg_embedding_backward", "fdg_recurrence_saved", "fdg_recurrence_forward",
+           "fdg_recurrence_backward", "fdg_distill_loss", "fdg_op_last_error",
            "fdg_last_error", "fdg_destroy"]
 
 
@@ -61,6 +63,18 @@ class fdg_options(C.Structure):
                 ("num_classes", C.c_int32), ("serial", C.c_int32), ("kernel_path", C.c_int32),
                 ("worker_groups", C.c_int32), ("streams", C.POINTER(C.c_void_p)), ("mixing", C.POINTER(C.c_double)),
                 ("grid_sms", C.c_int32)]
+
+
+class fdg_recurrence(C.Structure):
+    _fields_ = [("dtype", C.c_int32)] + [(n, C.c_int64) for n in (
+        "batch", "steps", "channels", "gate_batch", "gate_step", "value_batch", "value_step", "y_batch", "y_step", "dy_batch", "dy_step",
+        "dgate_batch", "dgate_step", "dvalue_batch", "dvalue_step")]
+
+
+class fdg_distill(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("logits_dtype", "dlogits_dtype", "top")] + \
+               [(n, C.c_int64) for n in ("rows", "vocab", "logits_stride", "dlogits_stride")] + \
+               [(n, C.c_float) for n in ("temperature", "weight", "scale")]
 
 
 _lib = None
@@ -118,6 +132,19 @@ def lib():
         L.fdg_bias_grad_static.argtypes = [vp, C.c_int32, C.c_int64, C.c_int32, vp, vp]
         L.fdg_static_last_error.restype = C.c_char_p
         L.fdg_static_last_error.argtypes = []
+        i32, i64, f32, size_p = C.c_int32, C.c_int64, C.c_float, C.POINTER(C.c_size_t)
+        rec, dis = C.POINTER(fdg_recurrence), C.POINTER(fdg_distill)
+        for name, args in (("fdg_embedding_forward", [vp, i64, vp, i32, i64, i64, f32, vp, i64, vp]),
+                           ("fdg_embedding_workspace", [i64, i64, i64, size_p]),
+                           ("fdg_embedding_backward", [vp, i64, vp, i32, i64, i64, i64, f32, i32, vp, vp, C.c_size_t, vp]),
+                           ("fdg_recurrence_saved", [rec, size_p]),
+                           ("fdg_recurrence_forward", [rec] + [vp] * 8),
+                           ("fdg_recurrence_backward", [rec] + [vp] * 10),
+                           ("fdg_distill_loss", [dis] + [vp] * 7)):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = args
+        L.fdg_op_last_error.restype = C.c_char_p
+        L.fdg_op_last_error.argtypes = []
         L.fdg_last_error.restype = C.c_char_p
         L.fdg_last_error.argtypes = [vp]
         L.fdg_destroy.restype = None

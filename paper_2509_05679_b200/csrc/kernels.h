@@ -186,6 +186,7 @@ enum KernelClass {
     KC_POOL_FWD, KC_POOL_BWD, KC_GAP_FWD, KC_GAP_BWD, KC_BN_FWD_STATS, KC_BN_FWD_APPLY, KC_BN_BWD_REDUCE, KC_BN_BWD_APPLY,
     KC_SOFTMAX_CE, KC_SGD, KC_TAGS, KC_FILL, KC_TC_FWD, KC_TC_DGRAD, KC_TC_WGRAD, KC_TC_AUX, KC_INGEST,
     KC_MMA_FWD, KC_MMA_DGRAD, KC_MMA_WGRAD,        // mconv.cu
+    KC_EMBED_FWD, KC_EMBED_GRAD, KC_RECUR_FWD, KC_RECUR_BWD, KC_DISTILL,        // embed.cu, recur.cu, distill.cu
     KC_COUNT
 };
 struct KernelStat { uint64_t launches; double ms, flops, bytes; };
