@@ -5,7 +5,6 @@
 // maps are found side by side and joined: a thread composes STEPS = 4 steps of four channels, a warp its threads by shuffles, the CTA its warps and, where
 // a launch would otherwise be too small, a cluster its CTAs through distributed shared memory; then every thread runs its steps again from the state in front of
 // them.  The joins are a fixed tree, so equal inputs give equal bits.  Backwards the same with g_t = a_t d_t, the map g -> a (g + dy).
-// The gate is computed twice (once to find the maps, once to apply them): the exponential and the reciprocal cost less than the registers that would hold it.
 //
 // Bound: HBM (forward 3 values a step and channel, backward 5).  A CTA walks along its sequence with a ring of tiles that cp.async fills ahead; a thread
 // reads only what it copied itself, so the ring needs no barrier.
@@ -36,27 +35,37 @@ template <int CX> struct Geo {
     static constexpr int RANKS = CX > 16 ? 1 : MAX_CLUSTER;
 };
 
-// a = sigmoid(z) and b = 1 - a = sigmoid(-z), each to a few units of its own last place; 0 and 1 at the infinities
-__device__ __forceinline__ void gate(float z, float& a, float& b) {
-    const float e = __expf(-fabsf(z));
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-    const float q = e * r;
-    a = z >= 0.f ? r : q;
-    b = z >= 0.f ? q : r;
+// Values go in pairs through the packed fp32 instructions: the kernels issue too much, not too little, to keep up with HBM.
+struct Four { float2 p[2]; };
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+
+// a = sigmoid(z) and q = 1 - a, each to a few units of its own last place: e = 2^min(-z log2 e, 100), a = 1 / (1 + e), q = e a.  Behind the bound a is 2^-100
+// instead of less and q is 1; NaN stays.
+__device__ __forceinline__ void gate(float2 z, float2& a, float2& q) {
+    const float2 t = mul(z, both(-1.4426950408889634f));
+    float2 e;
+    asm("min.NaN.f32 %0, %1, 0f42C80000;" : "=f"(e.x) : "f"(t.x));
+    asm("min.NaN.f32 %0, %1, 0f42C80000;" : "=f"(e.y) : "f"(t.y));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    const float2 d = __fadd2_rn(e, both(1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
+    q = mul(e, a);
 }
 
 template <typename T> struct Raw;                    // N values as they are stored
 template <> struct Raw<float> { using V = float4; };
 template <> struct Raw<bf16> { using V = uint2; };
-__device__ __forceinline__ void unpack(const float4& r, float* x) { x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w; }
-__device__ __forceinline__ void unpack(const uint2& r, float* x) {
-    x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
-    x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
+__device__ __forceinline__ Four unpack(const float4& r) { return {make_float2(r.x, r.y), make_float2(r.z, r.w)}; }
+__device__ __forceinline__ Four unpack(const uint2& r) {
+    return {make_float2(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u)), make_float2(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u))};
 }
-__device__ __forceinline__ void pack(const float* x, float4& r) { r = make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ void pack(const float* x, uint2& r) {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
+__device__ __forceinline__ void pack(const Four& x, float4& r) { r = make_float4(x.p[0].x, x.p[0].y, x.p[1].x, x.p[1].y); }
+__device__ __forceinline__ void pack(const Four& x, uint2& r) {
+    const __nv_bfloat162 lo = __float22bfloat162_rn(x.p[0]), hi = __float22bfloat162_rn(x.p[1]);
     r = make_uint2(*(const unsigned*)&lo, *(const unsigned*)&hi);
 }
 __device__ __forceinline__ float ld(const float* p) { return *p; }
@@ -74,116 +83,138 @@ template <int LEFT> __device__ __forceinline__ void copies_arrived() { asm volat
 template <typename T, int ACC> __device__ __forceinline__ void fetch(void* slot, const T* g, int left) {
     if constexpr (ACC * sizeof(T) >= 4) {
 #pragma unroll
-        for (int j = 0; j < N; j += ACC) if (j < left) copy_async<ACC * sizeof(T)>((T*)slot + j, g + j);
+        for (int j = 0; j < N; j += ACC) if (ACC == N || j < left) copy_async<ACC * sizeof(T)>((T*)slot + j, g + j);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j) if (j < left) ((T*)slot)[j] = g[j];
     }
 }
-template <typename T, int ACC> __device__ __forceinline__ void put(T* g, float* x, int left, bool accum) {
-    if (accum) for (int j = 0; j < N; ++j) if (j < left) x[j] += ld(g + j);
-    if constexpr (ACC == N) {
-        if (left > 0) { typename Raw<T>::V r; pack(x, r); *(typename Raw<T>::V*)g = r; }
-    } else if constexpr (ACC == 2) {
-        if (left > 0) *(__nv_bfloat162*)g = __floats2bfloat162_rn(x[0], x[1]);
-        if (left > 2) *(__nv_bfloat162*)(g + 2) = __floats2bfloat162_rn(x[2], x[3]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (j < left) st(g + j, x[j]);
+template <typename T, int ACC> __device__ __forceinline__ void put(T* g, Four x, int left, bool accum) {
+    if (accum) {
+        if (0 < left) x.p[0].x += ld(g);
+        if (1 < left) x.p[0].y += ld(g + 1);
+        if (2 < left) x.p[1].x += ld(g + 2);
+        if (3 < left) x.p[1].y += ld(g + 3);
     }
+    if constexpr (ACC == N) {
+        typename Raw<T>::V r;
+        pack(x, r);
+        *(typename Raw<T>::V*)g = r;
+    } else if constexpr (ACC == 2) {
+        *(__nv_bfloat162*)g = __float22bfloat162_rn(x.p[0]);
+        if (left > 2) *(__nv_bfloat162*)(g + 2) = __float22bfloat162_rn(x.p[1]);
+    } else {
+        st(g, x.p[0].x);
+        if (1 < left) st(g + 1, x.p[0].y);
+        if (2 < left) st(g + 2, x.p[1].x);
+        if (3 < left) st(g + 3, x.p[1].y);
+    }
+}
+// steps of t0 .. t0 + STEPS - 1 that lie in front of `end`
+__device__ __forceinline__ int steps_before(long end, long t0) {
+    const long n = end - t0;
+    return n <= 0 ? 0 : n < STEPS ? (int)n : STEPS;
 }
 
 template <typename T, int TENSORS> struct Ring {
     using V = typename Raw<T>::V;
-    static constexpr int STAGES = sizeof(T) == 2 ? (TENSORS == 2 ? 4 : 3) : 2;
-    static constexpr int BYTES = STAGES * STEPS * TENSORS * THREADS * (int)sizeof(V);
-    V* base;
-    __device__ V* slot(int stage, int i, int tensor) const { return base + ((stage * STEPS + i) * TENSORS + tensor) * THREADS + threadIdx.x; }
+    static constexpr int STAGES = sizeof(T) == 2 ? 3 : 2;
+    static constexpr int STAGE = STEPS * TENSORS * THREADS;
+    static constexpr int BYTES = STAGES * STAGE * (int)sizeof(V);
+    V* mine;                                                     // this thread's first slot
+    __device__ V* slot(int stage, int i, int tensor) const { return mine + stage * STAGE + (i * TENSORS + tensor) * THREADS; }
 };
 
-// (a1, h1), then (a2, h2)
-__device__ __forceinline__ void then(float a1, float h1, float a2, float h2, float& a, float& h) { h = fmaf(a2, h1, h2); a = a2 * a1; }
+// the map (a1, h1), then (a, h), in place of (a, h)
+__device__ __forceinline__ void after(float2 a1, float2 h1, float2& a, float2& h) { h = fma(a, h1, h); a = mul(a, a1); }
+__device__ __forceinline__ float2 shfl_up(float2 v, int d) { return make_float2(__shfl_up_sync(~0u, v.x, d), __shfl_up_sync(~0u, v.y, d)); }
+__device__ __forceinline__ float2 shfl_down(float2 v, int d) { return make_float2(__shfl_down_sync(~0u, v.x, d), __shfl_down_sync(~0u, v.y, d)); }
+// Over the step groups of a warp: (A, H) becomes the map of the groups up to and with this one, (Ax, Hx) that of those before it; UP: in the order of
+// the lanes, else against it.
+template <int CX, bool UP> __device__ __forceinline__ void join(Four& A, Four& H, Four& Ax, Four& Hx) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) { Ax.p[j] = both(1.f); Hx.p[j] = both(0.f); }
+#pragma unroll
+    for (int d = CX; d < 32; d *= 2)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float2 a = UP ? shfl_up(A.p[j], d) : shfl_down(A.p[j], d), h = UP ? shfl_up(H.p[j], d) : shfl_down(H.p[j], d);
+            if (UP ? lane >= d : lane < 32 - d) {
+                after(a, h, A.p[j], H.p[j]);
+                if (d == CX) { Ax.p[j] = a; Hx.p[j] = h; } else after(a, h, Ax.p[j], Hx.p[j]);
+            }
+        }
+}
+__device__ __forceinline__ void store(float* p, const Four& x) { *(float4*)p = make_float4(x.p[0].x, x.p[0].y, x.p[1].x, x.p[1].y); }
+__device__ __forceinline__ Four load(const float* p) { const float4 r = *(const float4*)p; return {make_float2(r.x, r.y), make_float2(r.z, r.w)}; }
 
 template <typename T, int ACC, int CX>
-__global__ void __launch_bounds__(THREADS) recur_fwd_k(RecurArgs p, int R, int slices) {
+__global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, int slices) {
     using G = Geo<CX>;
+    using Rg = Ring<T, 2>;
     extern __shared__ __align__(16) char dyn[];
-    const Ring<T, 2> ring{(typename Raw<T>::V*)dyn};
-    constexpr int STAGES = Ring<T, 2>::STAGES;
+    const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
     __shared__ __align__(16) float tot_a[G::TEAMS][G::CH], tot_h[G::TEAMS][G::CH], in_h[G::TEAMS][G::CH];
     __shared__ float2 joined[2][G::RANKS][G::CH];
     const int rank = R > 1 ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
-    const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM;
+    const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM, lane = threadIdx.x & 31;
     const long c = c0 + cx * N;
     const int left = (int)min((long)N, p.C - c);                 // channels of this thread that exist
-    const T* const z = (const T*)p.z + b * p.z_b + c;
-    const T* const v = (const T*)p.v + b * p.v_b + c;
-    T* const y = (T*)p.y + b * p.y_b + c;
     const long len = p.lengths ? min((long)max(p.lengths[b], 0), p.T) : p.T;
-    const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R;
-    auto fetch_tile = [&](long round) {
-        if (round < rounds) {
-            const long t0 = (round * R + rank) * G::TILE + tg * STEPS;
+    const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = (long)R * G::TILE;
+    long t0 = (long)rank * G::TILE + tg * STEPS, tf = t0;        // this thread's first step: of the round, of the next tile to fetch
+    const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
+    const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
+    T* y = (T*)p.y + b * p.y_b + c + t0 * p.y_t;
+    auto fetch_tile = [&](int stage) {
+        const int n = left > 0 ? steps_before(len, tf) : 0;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i)
-                if (t0 + i < len) {
-                    fetch<T, ACC>(ring.slot((int)(round % STAGES), i, 0), z + (t0 + i) * p.z_t, left);
-                    fetch<T, ACC>(ring.slot((int)(round % STAGES), i, 1), v + (t0 + i) * p.v_t, left);
-                }
-        }
+        for (int i = 0; i < STEPS; ++i)
+            if (i < n) {
+                fetch<T, ACC>(ring.slot(stage, i, 0), zf + i * p.z_t, left);
+                fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
+            }
         copies_issued();
+        tf += stride; zf += stride * p.z_t; vf += stride * p.v_t;
     };
-    for (int s = 0; s < STAGES - 1; ++s) fetch_tile(s);
+    for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
     const bool keeper = threadIdx.x < G::CH;                     // one thread per channel joins the teams
     const long kc = c0 + threadIdx.x;
     float carry = keeper && kc < p.C && p.state ? p.state[b * p.C + kc] : 0.f;
+    const bool saves = p.saved && keeper && kc < p.C;
+    int stage = 0;
     for (long round = 0; round < rounds; ++round) {
-        fetch_tile(round + STAGES - 1);
-        copies_arrived<STAGES - 1>();
-        const int stage = (int)(round % STAGES);
-        const long tile = round * R + rank, t0 = tile * G::TILE + tg * STEPS;
+        fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
+        copies_arrived<Rg::STAGES - 1>();
         // the map of this thread's steps
-        float A[N] = {1.f, 1.f, 1.f, 1.f}, H[N] = {};
+        const int n = steps_before(len, t0);
+        Four a[STEPS], u[STEPS], A, H, Ax, Hx;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-            if (t0 + i < len) {
-                float zz[N], vv[N];
-                unpack(*ring.slot(stage, i, 0), zz); unpack(*ring.slot(stage, i, 1), vv);
+        for (int i = 0; i < STEPS; ++i) {
+            const Four z = unpack(*ring.slot(stage, i, 0)), v = unpack(*ring.slot(stage, i, 1));
 #pragma unroll
-                for (int j = 0; j < N; ++j) { float a, q; gate(zz[j], a, q); H[j] = fmaf(a, H[j], q * vv[j]); A[j] *= a; }
+            for (int j = 0; j < 2; ++j) {
+                float2 q;
+                gate(z.p[j], a[i].p[j], q);
+                u[i].p[j] = mul(q, v.p[j]);
+                if (i >= n) { a[i].p[j] = both(1.f); u[i].p[j] = both(0.f); }
+                if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u[0].p[j]; }
+                else { H.p[j] = fma(a[i].p[j], H.p[j], u[i].p[j]); A.p[j] = mul(A.p[j], a[i].p[j]); }
             }
-        // of the threads in front of it in its team, and the team's
-        float Ax[N], Hx[N];
-        if constexpr (CX < 32) {
-#pragma unroll
-            for (int d = CX; d < 32; d *= 2)
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float a = __shfl_up_sync(~0u, A[j], d), h = __shfl_up_sync(~0u, H[j], d);
-                    if ((int)(threadIdx.x & 31) >= d) then(a, h, A[j], H[j], A[j], H[j]);
-                }
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                Ax[j] = __shfl_up_sync(~0u, A[j], CX); Hx[j] = __shfl_up_sync(~0u, H[j], CX);
-                if ((int)(threadIdx.x & 31) < CX) { Ax[j] = 1.f; Hx[j] = 0.f; }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j) { Ax[j] = 1.f; Hx[j] = 0.f; }
         }
-        if (CX >= 32 || (int)(threadIdx.x & 31) >= 32 - CX) {
-            *(float4*)&tot_a[team][cx * N] = make_float4(A[0], A[1], A[2], A[3]);
-            *(float4*)&tot_h[team][cx * N] = make_float4(H[0], H[1], H[2], H[3]);
-        }
+        join<CX, true>(A, H, Ax, Hx);                            // of the threads in front of it in its team, and the team's
+        if (CX >= 32 || lane >= 32 - CX) { store(&tot_a[team][cx * N], A); store(&tot_h[team][cx * N], H); }
         __syncthreads();
         if (R > 1) {                                             // the CTA's map goes to every CTA of the cluster
             cg::cluster_group cl = cg::this_cluster();
             if (keeper) {
-                float a = 1.f, h = 0.f;
-                for (int w = 0; w < G::TEAMS; ++w) then(a, h, tot_a[w][threadIdx.x], tot_h[w][threadIdx.x], a, h);
-                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[round & 1][rank][threadIdx.x], r) = make_float2(a, h);
+                float ta = 1.f, th = 0.f;
+#pragma unroll
+                for (int w = 0; w < G::TEAMS; ++w) { th = fmaf(tot_a[w][threadIdx.x], th, tot_h[w][threadIdx.x]); ta *= tot_a[w][threadIdx.x]; }
+                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[round & 1][rank][threadIdx.x], r) = make_float2(ta, th);
             }
             cl.sync();
         }
@@ -195,39 +226,35 @@ __global__ void __launch_bounds__(THREADS) recur_fwd_k(RecurArgs p, int R, int s
                     if (r == rank) h = carry;
                     carry = fmaf(m.x, carry, m.y);
                 }
-            if (p.saved && kc < p.C && tile < tiles) p.saved[(b * tiles + tile) * p.C + kc] = h;
+            if (saves && round * R + rank < tiles) p.saved[(b * tiles + round * R + rank) * p.C + kc] = h;
+#pragma unroll
             for (int w = 0; w < G::TEAMS; ++w) { in_h[w][threadIdx.x] = h; h = fmaf(tot_a[w][threadIdx.x], h, tot_h[w][threadIdx.x]); }
             if (R == 1) carry = h;
         }
         __syncthreads();
-        float h[N];
-        {
-            const float4 q = *(const float4*)&in_h[team][cx * N];
-            h[0] = fmaf(Ax[0], q.x, Hx[0]); h[1] = fmaf(Ax[1], q.y, Hx[1]); h[2] = fmaf(Ax[2], q.z, Hx[2]); h[3] = fmaf(Ax[3], q.w, Hx[3]);
-        }
+        Four h = load(&in_h[team][cx * N]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) h.p[j] = fma(Ax.p[j], h.p[j], Hx.p[j]);
+        const int out = left > 0 ? steps_before(p.T, t0) : 0;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            if (t0 + i >= p.T) break;
-            float o[N] = {};
-            if (t0 + i < len) {
-                float zz[N], vv[N];
-                unpack(*ring.slot(stage, i, 0), zz); unpack(*ring.slot(stage, i, 1), vv);
 #pragma unroll
-                for (int j = 0; j < N; ++j) { float a, q; gate(zz[j], a, q); o[j] = h[j] = fmaf(a, h[j], q * vv[j]); }
-            }
-            put<T, ACC>(y + (t0 + i) * p.y_t, o, left, false);
+            for (int j = 0; j < 2; ++j) h.p[j] = fma(a[i].p[j], h.p[j], u[i].p[j]);
+            if (i < out) put<T, ACC>(y + i * p.y_t, i < n ? h : Four{}, left, false);
         }
+        t0 += stride; y += stride * p.y_t;
+        stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
     if (p.state_out && keeper && rank == 0 && kc < p.C) p.state_out[b * p.C + kc] = carry;
     if (R > 1) cg::this_cluster().sync();                        // nobody leaves while others may write to its shared memory
 }
 
 template <typename T, int ACC, int CX>
-__global__ void __launch_bounds__(THREADS) recur_bwd_k(RecurArgs p, int R, int slices) {
+__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, int slices) {
     using G = Geo<CX>;
+    using Rg = Ring<T, 3>;
     extern __shared__ __align__(16) char dyn[];
-    const Ring<T, 3> ring{(typename Raw<T>::V*)dyn};
-    constexpr int STAGES = Ring<T, 3>::STAGES;
+    const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
     __shared__ __align__(16) float tot_a[G::TEAMS][G::CH], tot_h[G::TEAMS][G::CH], tot_g[G::TEAMS][G::CH], in_h[G::TEAMS][G::CH], in_g[G::TEAMS][G::CH];
     __shared__ float2 joined[2][G::RANKS][G::CH];
     const int rank = R > 1 ? (int)(blockIdx.x % R) : 0;
@@ -236,90 +263,69 @@ __global__ void __launch_bounds__(THREADS) recur_bwd_k(RecurArgs p, int R, int s
     const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM, lane = threadIdx.x & 31;
     const long c = c0 + cx * N;
     const int left = (int)min((long)N, p.C - c);
-    const T* const z = (const T*)p.z + b * p.z_b + c;
-    const T* const v = (const T*)p.v + b * p.v_b + c;
-    const T* const dy = (const T*)p.dy + b * p.dy_b + c;
-    T* const dz = (T*)p.dz + b * p.dz_b + c;
-    T* const dv = (T*)p.dv + b * p.dv_b + c;
     const long len = p.lengths ? min((long)max(p.lengths[b], 0), p.T) : p.T;
-    const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R;
-    // rounds are counted from the end of the sequence
-    auto fetch_tile = [&](long round) {
-        if (round < rounds) {
-            const long t0 = ((rounds - 1 - round) * R + rank) * G::TILE + tg * STEPS;
-            const int stage = (int)(round % STAGES);
+    const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = (long)R * G::TILE;
+    // rounds go from the end of the sequence to its beginning
+    const long last = (rounds - 1) * R + rank;                   // the first round's tile
+    long t0 = last * G::TILE + tg * STEPS, tf = t0;
+    const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
+    const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
+    const T* df = (const T*)p.dy + b * p.dy_b + c + t0 * p.dy_t;
+    T* dz = (T*)p.dz + b * p.dz_b + c + t0 * p.dz_t;
+    T* dv = (T*)p.dv + b * p.dv_b + c + t0 * p.dv_t;
+    auto fetch_tile = [&](int stage) {
+        const int n = left > 0 && tf >= 0 ? steps_before(len, tf) : 0;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i)
-                if (t0 + i < len) {
-                    fetch<T, ACC>(ring.slot(stage, i, 0), z + (t0 + i) * p.z_t, left);
-                    fetch<T, ACC>(ring.slot(stage, i, 1), v + (t0 + i) * p.v_t, left);
-                    fetch<T, ACC>(ring.slot(stage, i, 2), dy + (t0 + i) * p.dy_t, left);
-                }
-        }
+        for (int i = 0; i < STEPS; ++i)
+            if (i < n) {
+                fetch<T, ACC>(ring.slot(stage, i, 0), zf + i * p.z_t, left);
+                fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
+                fetch<T, ACC>(ring.slot(stage, i, 2), df + i * p.dy_t, left);
+            }
         copies_issued();
+        tf -= stride; zf -= stride * p.z_t; vf -= stride * p.v_t; df -= stride * p.dy_t;
     };
-    for (int s = 0; s < STAGES - 1; ++s) fetch_tile(s);
+    for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
     const bool keeper = threadIdx.x < G::CH;
     const long kc = c0 + threadIdx.x;
     float carry = keeper && kc < p.C && p.dstate_out ? p.dstate_out[b * p.C + kc] : 0.f;
+    int stage = 0;
     for (long round = 0; round < rounds; ++round) {
-        fetch_tile(round + STAGES - 1);
-        const long tile = (rounds - 1 - round) * R + rank, t0 = tile * G::TILE + tg * STEPS;
+        fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
+        const long tile = last - round * R;
         const float start = keeper && kc < p.C && tile < tiles ? p.saved[(b * tiles + tile) * p.C + kc] : 0.f;
-        copies_arrived<STAGES - 1>();
-        const int stage = (int)(round % STAGES);
-        float A[N] = {1.f, 1.f, 1.f, 1.f}, H[N] = {}, Q[N] = {};
+        copies_arrived<Rg::STAGES - 1>();
+        const int n = steps_before(len, t0);
+        Four a[STEPS], q[STEPS], A, B, H, Q, Ax, Hx, Ay, Qy;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-            if (t0 + i < len) {
-                float zz[N], vv[N], dd[N];
-                unpack(*ring.slot(stage, i, 0), zz); unpack(*ring.slot(stage, i, 1), vv); unpack(*ring.slot(stage, i, 2), dd);
+        for (int i = 0; i < STEPS; ++i) {
+            const Four z = unpack(*ring.slot(stage, i, 0)), v = unpack(*ring.slot(stage, i, 1)), d = unpack(*ring.slot(stage, i, 2));
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    float a, q;
-                    gate(zz[j], a, q);
-                    H[j] = fmaf(a, H[j], q * vv[j]);
-                    A[j] *= a;
-                    Q[j] = fmaf(A[j], dd[j], Q[j]);             // what dy of this step is in front of the thread's first one
+            for (int j = 0; j < 2; ++j) {
+                gate(z.p[j], a[i].p[j], q[i].p[j]);
+                float2 u = mul(q[i].p[j], v.p[j]), e = d.p[j];
+                if (i >= n) { a[i].p[j] = both(1.f); u = e = both(0.f); }
+                if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u; Q.p[j] = mul(A.p[j], e); }
+                else {
+                    H.p[j] = fma(a[i].p[j], H.p[j], u);
+                    A.p[j] = mul(A.p[j], a[i].p[j]);
+                    Q.p[j] = fma(A.p[j], e, Q.p[j]);             // what dy of this step is in front of the thread's first one
                 }
             }
-        float Ax[N], Hx[N], Ay[N], Qy[N];                        // of the threads in front (forward map) and behind (backward map)
-        if constexpr (CX < 32) {
-            float B[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) B[j] = A[j];
-#pragma unroll
-            for (int d = CX; d < 32; d *= 2)
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float a = __shfl_up_sync(~0u, A[j], d), h = __shfl_up_sync(~0u, H[j], d);
-                    if (lane >= d) then(a, h, A[j], H[j], A[j], H[j]);
-                    const float e = __shfl_down_sync(~0u, B[j], d), q = __shfl_down_sync(~0u, Q[j], d);
-                    if (lane < 32 - d) then(e, q, B[j], Q[j], B[j], Q[j]);
-                }
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                Ax[j] = __shfl_up_sync(~0u, A[j], CX); Hx[j] = __shfl_up_sync(~0u, H[j], CX);
-                Ay[j] = __shfl_down_sync(~0u, B[j], CX); Qy[j] = __shfl_down_sync(~0u, Q[j], CX);
-                if (lane < CX) { Ax[j] = 1.f; Hx[j] = 0.f; }
-                if (lane >= 32 - CX) { Ay[j] = 1.f; Qy[j] = 0.f; }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j) { Ax[j] = Ay[j] = 1.f; Hx[j] = Qy[j] = 0.f; }
         }
-        if (CX >= 32 || lane >= 32 - CX) {
-            *(float4*)&tot_a[team][cx * N] = make_float4(A[0], A[1], A[2], A[3]);
-            *(float4*)&tot_h[team][cx * N] = make_float4(H[0], H[1], H[2], H[3]);
-        }
-        if (CX >= 32 || lane < CX) *(float4*)&tot_g[team][cx * N] = make_float4(Q[0], Q[1], Q[2], Q[3]);
+        B = A;
+        join<CX, true>(A, H, Ax, Hx);                            // of the threads in front (forward map)
+        join<CX, false>(B, Q, Ay, Qy);                           // and behind (backward map)
+        if (CX >= 32 || lane >= 32 - CX) { store(&tot_a[team][cx * N], A); store(&tot_h[team][cx * N], H); }
+        if (CX >= 32 || lane < CX) store(&tot_g[team][cx * N], Q);
         __syncthreads();
         if (R > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (keeper) {
-                float a = 1.f, g = 0.f;
-                for (int w = G::TEAMS - 1; w >= 0; --w) then(a, g, tot_a[w][threadIdx.x], tot_g[w][threadIdx.x], a, g);
-                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[round & 1][rank][threadIdx.x], r) = make_float2(a, g);
+                float ta = 1.f, tq = 0.f;
+#pragma unroll
+                for (int w = G::TEAMS - 1; w >= 0; --w) { tq = fmaf(tot_a[w][threadIdx.x], tq, tot_g[w][threadIdx.x]); ta *= tot_a[w][threadIdx.x]; }
+                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[round & 1][rank][threadIdx.x], r) = make_float2(ta, tq);
             }
             cl.sync();
         }
@@ -331,48 +337,49 @@ __global__ void __launch_bounds__(THREADS) recur_bwd_k(RecurArgs p, int R, int s
                     if (r == rank) g = carry;
                     carry = fmaf(m.x, carry, m.y);
                 }
+#pragma unroll
             for (int w = 0; w < G::TEAMS; ++w) {
-                const int u = G::TEAMS - 1 - w;
+                const int x = G::TEAMS - 1 - w;
                 in_h[w][threadIdx.x] = h; h = fmaf(tot_a[w][threadIdx.x], h, tot_h[w][threadIdx.x]);
-                in_g[u][threadIdx.x] = g; g = fmaf(tot_a[u][threadIdx.x], g, tot_g[u][threadIdx.x]);
+                in_g[x][threadIdx.x] = g; g = fmaf(tot_a[x][threadIdx.x], g, tot_g[x][threadIdx.x]);
             }
             if (R == 1) carry = g;
         }
         __syncthreads();
-        float g[N], a[STEPS][N], q[STEPS][N], before[STEPS][N];
-        {
-            const float4 x = *(const float4*)&in_h[team][cx * N], w = *(const float4*)&in_g[team][cx * N];
-            before[0][0] = fmaf(Ax[0], x.x, Hx[0]); before[0][1] = fmaf(Ax[1], x.y, Hx[1]); before[0][2] = fmaf(Ax[2], x.z, Hx[2]); before[0][3] = fmaf(Ax[3], x.w, Hx[3]);
-            g[0] = fmaf(Ay[0], w.x, Qy[0]); g[1] = fmaf(Ay[1], w.y, Qy[1]); g[2] = fmaf(Ay[2], w.z, Qy[2]); g[3] = fmaf(Ay[3], w.w, Qy[3]);
+        Four g = load(&in_g[team][cx * N]), before[STEPS];
+        before[0] = load(&in_h[team][cx * N]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            before[0].p[j] = fma(Ax.p[j], before[0].p[j], Hx.p[j]);
+            g.p[j] = fma(Ay.p[j], g.p[j], Qy.p[j]);
         }
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            float zz[N], vv[N];
-            unpack(*ring.slot(stage, i, 0), zz); unpack(*ring.slot(stage, i, 1), vv);
+        for (int i = 0; i + 1 < STEPS; ++i) {
+            const Four v = unpack(*ring.slot(stage, i, 1));
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                gate(zz[j], a[i][j], q[i][j]);
-                if (i + 1 < STEPS) before[i + 1][j] = fmaf(a[i][j], before[i][j], q[i][j] * vv[j]);
-            }
+            for (int j = 0; j < 2; ++j) before[i + 1].p[j] = fma(a[i].p[j], before[i].p[j], mul(q[i].p[j], v.p[j]));
         }
+        const int out = left > 0 ? steps_before(p.T, t0) : 0;
 #pragma unroll
         for (int i = STEPS - 1; i >= 0; --i) {
-            if (t0 + i >= p.T) continue;
-            float oz[N] = {}, ov[N] = {};
-            if (t0 + i < len) {
-                float vv[N], dd[N];
-                unpack(*ring.slot(stage, i, 1), vv); unpack(*ring.slot(stage, i, 2), dd);
+            const Four v = unpack(*ring.slot(stage, i, 1)), e = unpack(*ring.slot(stage, i, 2));
+            Four oz{}, ov{};
+            if (i < n) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float d = dd[j] + g[j];
-                    ov[j] = q[i][j] * d;
-                    oz[j] = a[i][j] * ov[j] * (before[i][j] - vv[j]);
-                    g[j] = a[i][j] * d;
+                for (int j = 0; j < 2; ++j) {
+                    const float2 d = __fadd2_rn(e.p[j], g.p[j]);
+                    ov.p[j] = mul(q[i].p[j], d);
+                    oz.p[j] = mul(mul(a[i].p[j], ov.p[j]), fma(v.p[j], both(-1.f), before[i].p[j]));
+                    g.p[j] = mul(a[i].p[j], d);
                 }
             }
-            put<T, ACC>(dz + (t0 + i) * p.dz_t, oz, left, p.accum);
-            put<T, ACC>(dv + (t0 + i) * p.dv_t, ov, left, p.accum);
+            if (i < out) {
+                put<T, ACC>(dz + i * p.dz_t, oz, left, p.accum);
+                put<T, ACC>(dv + i * p.dv_t, ov, left, p.accum);
+            }
         }
+        t0 -= stride; dz -= stride * p.dz_t; dv -= stride * p.dv_t;
+        stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
     if (p.dstate && keeper && rank == 0 && kc < p.C) p.dstate[b * p.C + kc] = carry;
     if (R > 1) cg::this_cluster().sync();
