@@ -68,6 +68,9 @@ __device__ __forceinline__ void pack(const Four& x, uint2& r) {
     const __nv_bfloat162 lo = __float22bfloat162_rn(x.p[0]), hi = __float22bfloat162_rn(x.p[1]);
     r = make_uint2(*(const unsigned*)&lo, *(const unsigned*)&hi);
 }
+// a step that changes nothing: gate open (+infinity), value and dy zero
+__device__ __forceinline__ void idle(float4* z, float4* x) { *z = make_float4(INFINITY, INFINITY, INFINITY, INFINITY); *x = make_float4(0.f, 0.f, 0.f, 0.f); }
+__device__ __forceinline__ void idle(uint2* z, uint2* x) { *z = make_uint2(0x7f807f80u, 0x7f807f80u); *x = make_uint2(0u, 0u); }
 __device__ __forceinline__ float ld(const float* p) { return *p; }
 __device__ __forceinline__ float ld(const bf16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
@@ -146,17 +149,53 @@ template <int CX, bool UP> __device__ __forceinline__ void join(Four& A, Four& H
             }
         }
 }
-__device__ __forceinline__ void store(float* p, const Four& x) { *(float4*)p = make_float4(x.p[0].x, x.p[0].y, x.p[1].x, x.p[1].y); }
-__device__ __forceinline__ Four load(const float* p) { const float4 r = *(const float4*)p; return {make_float2(r.x, r.y), make_float2(r.z, r.w)}; }
+// Maps of the teams, one {A, H} per channel.
+__device__ __forceinline__ void store(float2* p, const Four& A, const Four& H) {
+    *(float4*)p = make_float4(A.p[0].x, H.p[0].x, A.p[0].y, H.p[0].y);
+    *(float4*)(p + 2) = make_float4(A.p[1].x, H.p[1].x, A.p[1].y, H.p[1].y);
+}
+// The value that stands in front of a warp, for the channels of its lanes, from values and maps per channel.  Up to 32 channels a lane takes one channel
+// through the maps and the lanes exchange them; above, every lane takes its own four.
+template <int CX> struct Lanes {
+    static constexpr bool ONE = CX * N <= 32;
+    static constexpr int M = ONE ? 1 : N;
+    float v[M];
+    static __device__ __forceinline__ int first() { return ONE ? (threadIdx.x & 31) % (CX * N) : threadIdx.x % CX * N; }
+    __device__ __forceinline__ void set(const float* p) {
+        if constexpr (ONE) v[0] = *p;
+        else { const float4 r = *(const float4*)p; v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
+    }
+    __device__ __forceinline__ void through(const float2* p) {
+        if constexpr (ONE) { const float2 m = *p; v[0] = fmaf(m.x, v[0], m.y); }
+        else {
+            const float4 m = *(const float4*)p, k = *(const float4*)(p + 2);
+            v[0] = fmaf(m.x, v[0], m.y); v[1] = fmaf(m.z, v[1], m.w); v[2] = fmaf(k.x, v[2], k.y); v[3] = fmaf(k.z, v[3], k.w);
+        }
+    }
+    __device__ __forceinline__ Four four() const {
+        if constexpr (ONE) {
+            const int l = threadIdx.x % CX * N;
+            return {make_float2(__shfl_sync(~0u, v[0], l), __shfl_sync(~0u, v[0], l + 1)), make_float2(__shfl_sync(~0u, v[0], l + 2), __shfl_sync(~0u, v[0], l + 3))};
+        } else return {make_float2(v[0], v[1]), make_float2(v[2], v[3])};
+    }
+};
+// values of channels first .. of a row of C, zero behind its end
+template <int CX> __device__ __forceinline__ void read(Lanes<CX>& l, const float* row, long first, long C) {
+#pragma unroll
+    for (int j = 0; j < Lanes<CX>::M; ++j) l.v[j] = row && first + j < C ? row[first + j] : 0.f;
+}
 
+// One barrier a tile: behind it a warp goes through the maps of the teams in front of it by itself, and the last steps' threads leave the state for the
+// next tile, which the next tile's barrier orders.  What stands there is kept twice, by the round's parity.
 template <typename T, int ACC, int CX>
 __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, int slices) {
     using G = Geo<CX>;
     using Rg = Ring<T, 2>;
     extern __shared__ __align__(16) char dyn[];
     const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
-    __shared__ __align__(16) float tot_a[G::TEAMS][G::CH], tot_h[G::TEAMS][G::CH], in_h[G::TEAMS][G::CH];
-    __shared__ float2 joined[2][G::RANKS][G::CH];
+    __shared__ __align__(16) float2 tot[2][G::TEAMS][G::CH];
+    __shared__ __align__(16) float carried[2][G::CH];
+    __shared__ __align__(16) float2 joined[2][G::RANKS][G::CH];
     const int rank = R > 1 ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
@@ -176,21 +215,22 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
             if (i < n) {
                 fetch<T, ACC>(ring.slot(stage, i, 0), zf + i * p.z_t, left);
                 fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
-            }
+            } else idle(ring.slot(stage, i, 0), ring.slot(stage, i, 1));
         copies_issued();
         tf += stride; zf += stride * p.z_t; vf += stride * p.v_t;
     };
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
-    const bool keeper = threadIdx.x < G::CH;                     // one thread per channel joins the teams
-    const long kc = c0 + threadIdx.x;
-    float carry = keeper && kc < p.C && p.state ? p.state[b * p.C + kc] : 0.f;
-    const bool saves = p.saved && keeper && kc < p.C;
+    if (R > 1) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
+    const int first = Lanes<CX>::first();
+    Lanes<CX> carry;                                             // R > 1: the state in front of the round, in every warp
+    read<CX>(carry, p.state ? p.state + b * p.C : nullptr, c0 + first, p.C);
+    if (threadIdx.x < G::CH) carried[0][threadIdx.x] = p.state && c0 + threadIdx.x < p.C ? p.state[b * p.C + c0 + threadIdx.x] : 0.f;
     int stage = 0;
     for (long round = 0; round < rounds; ++round) {
+        const int now = (int)(round & 1);
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
         copies_arrived<Rg::STAGES - 1>();
         // the map of this thread's steps
-        const int n = steps_before(len, t0);
         Four a[STEPS], u[STEPS], A, H, Ax, Hx;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
@@ -200,53 +240,64 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
                 float2 q;
                 gate(z.p[j], a[i].p[j], q);
                 u[i].p[j] = mul(q, v.p[j]);
-                if (i >= n) { a[i].p[j] = both(1.f); u[i].p[j] = both(0.f); }
                 if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u[0].p[j]; }
                 else { H.p[j] = fma(a[i].p[j], H.p[j], u[i].p[j]); A.p[j] = mul(A.p[j], a[i].p[j]); }
             }
         }
         join<CX, true>(A, H, Ax, Hx);                            // of the threads in front of it in its team, and the team's
-        if (CX >= 32 || lane >= 32 - CX) { store(&tot_a[team][cx * N], A); store(&tot_h[team][cx * N], H); }
+        if (CX >= 32 || lane >= 32 - CX) store(&tot[now][team][cx * N], A, H);
         __syncthreads();
+        Lanes<CX> in;
         if (R > 1) {                                             // the CTA's map goes to every CTA of the cluster
             cg::cluster_group cl = cg::this_cluster();
-            if (keeper) {
+            if (threadIdx.x < G::CH) {
                 float ta = 1.f, th = 0.f;
 #pragma unroll
-                for (int w = 0; w < G::TEAMS; ++w) { th = fmaf(tot_a[w][threadIdx.x], th, tot_h[w][threadIdx.x]); ta *= tot_a[w][threadIdx.x]; }
-                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[round & 1][rank][threadIdx.x], r) = make_float2(ta, th);
+                for (int w = 0; w < G::TEAMS; ++w) { const float2 m = tot[now][w][threadIdx.x]; th = fmaf(m.x, th, m.y); ta *= m.x; }
+                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[now][rank][threadIdx.x], r) = make_float2(ta, th);
             }
             cl.sync();
-        }
-        if (keeper) {
-            float h = carry;
-            if (R > 1)
-                for (int r = 0; r < R; ++r) {
-                    const float2 m = joined[round & 1][r][threadIdx.x];
-                    if (r == rank) h = carry;
-                    carry = fmaf(m.x, carry, m.y);
-                }
-            if (saves && round * R + rank < tiles) p.saved[(b * tiles + round * R + rank) * p.C + kc] = h;
+            for (int r = 0; r < R; ++r) {
+                if (r == rank) in = carry;
+                carry.through(&joined[now][r][first]);
+            }
+        } else in.set(&carried[now][first]);
+        if (p.saved && threadIdx.x < G::TEAM && (!Lanes<CX>::ONE || lane < G::CH) && (Lanes<CX>::ONE || CX >= 32 || lane < CX)) {
+            const long tile = round * R + rank;
 #pragma unroll
-            for (int w = 0; w < G::TEAMS; ++w) { in_h[w][threadIdx.x] = h; h = fmaf(tot_a[w][threadIdx.x], h, tot_h[w][threadIdx.x]); }
-            if (R == 1) carry = h;
+            for (int j = 0; j < Lanes<CX>::M; ++j) if (tile < tiles && c0 + first + j < p.C) p.saved[(b * tiles + tile) * p.C + c0 + first + j] = in.v[j];
         }
-        __syncthreads();
-        Four h = load(&in_h[team][cx * N]);
+        for (int w = 0; w < team; ++w) in.through(&tot[now][w][first]);
+        Four h = in.four();
 #pragma unroll
         for (int j = 0; j < 2; ++j) h.p[j] = fma(Ax.p[j], h.p[j], Hx.p[j]);
-        const int out = left > 0 ? steps_before(p.T, t0) : 0;
+        const int n = left > 0 ? steps_before(len, t0) : 0;
+        if (n == STEPS) {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
+            for (int i = 0; i < STEPS; ++i) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) h.p[j] = fma(a[i].p[j], h.p[j], u[i].p[j]);
-            if (i < out) put<T, ACC>(y + i * p.y_t, i < n ? h : Four{}, left, false);
+                for (int j = 0; j < 2; ++j) h.p[j] = fma(a[i].p[j], h.p[j], u[i].p[j]);
+                put<T, ACC>(y + i * p.y_t, h, left, false);
+            }
+        } else {
+            const int out = left > 0 ? steps_before(p.T, t0) : 0;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) h.p[j] = fma(a[i].p[j], h.p[j], u[i].p[j]);
+                if (i < out) put<T, ACC>(y + i * p.y_t, i < n ? h : Four{}, left, false);
+            }
         }
+        if (R == 1 && tg == G::TG - 1) *(float4*)&carried[now ^ 1][cx * N] = make_float4(h.p[0].x, h.p[0].y, h.p[1].x, h.p[1].y);
         t0 += stride; y += stride * p.y_t;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    if (p.state_out && keeper && rank == 0 && kc < p.C) p.state_out[b * p.C + kc] = carry;
     if (R > 1) cg::this_cluster().sync();                        // nobody leaves while others may write to its shared memory
+    else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
+    if (p.state_out && rank == 0 && threadIdx.x < G::TEAM) {
+#pragma unroll
+        for (int j = 0; j < Lanes<CX>::M; ++j) if (c0 + first + j < p.C) p.state_out[b * p.C + c0 + first + j] = carry.v[j];
+    }
 }
 
 template <typename T, int ACC, int CX>
@@ -255,8 +306,9 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
     using Rg = Ring<T, 3>;
     extern __shared__ __align__(16) char dyn[];
     const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
-    __shared__ __align__(16) float tot_a[G::TEAMS][G::CH], tot_h[G::TEAMS][G::CH], tot_g[G::TEAMS][G::CH], in_h[G::TEAMS][G::CH], in_g[G::TEAMS][G::CH];
-    __shared__ float2 joined[2][G::RANKS][G::CH];
+    __shared__ __align__(16) float2 tot_h[2][G::TEAMS][G::CH], tot_g[2][G::TEAMS][G::CH];
+    __shared__ __align__(16) float carried[2][G::CH];
+    __shared__ __align__(16) float2 joined[2][G::RANKS][G::CH];
     const int rank = R > 1 ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
@@ -266,8 +318,8 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
     const long len = p.lengths ? min((long)max(p.lengths[b], 0), p.T) : p.T;
     const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = (long)R * G::TILE;
     // rounds go from the end of the sequence to its beginning
-    const long last = (rounds - 1) * R + rank;                   // the first round's tile
-    long t0 = last * G::TILE + tg * STEPS, tf = t0;
+    long tile = (rounds - 1) * R + rank;
+    long t0 = tile * G::TILE + tg * STEPS, tf = t0;
     const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
     const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
     const T* df = (const T*)p.dy + b * p.dy_b + c + t0 * p.dy_t;
@@ -281,21 +333,26 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
                 fetch<T, ACC>(ring.slot(stage, i, 0), zf + i * p.z_t, left);
                 fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
                 fetch<T, ACC>(ring.slot(stage, i, 2), df + i * p.dy_t, left);
+            } else {
+                idle(ring.slot(stage, i, 0), ring.slot(stage, i, 1));
+                *ring.slot(stage, i, 2) = *ring.slot(stage, i, 1);
             }
         copies_issued();
         tf -= stride; zf -= stride * p.z_t; vf -= stride * p.v_t; df -= stride * p.dy_t;
     };
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
-    const bool keeper = threadIdx.x < G::CH;
-    const long kc = c0 + threadIdx.x;
-    float carry = keeper && kc < p.C && p.dstate_out ? p.dstate_out[b * p.C + kc] : 0.f;
+    if (R > 1) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
+    const int first = Lanes<CX>::first();
+    Lanes<CX> carry;
+    read<CX>(carry, p.dstate_out ? p.dstate_out + b * p.C : nullptr, c0 + first, p.C);
+    if (threadIdx.x < G::CH) carried[0][threadIdx.x] = p.dstate_out && c0 + threadIdx.x < p.C ? p.dstate_out[b * p.C + c0 + threadIdx.x] : 0.f;
     int stage = 0;
     for (long round = 0; round < rounds; ++round) {
+        const int now = (int)(round & 1);
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
-        const long tile = last - round * R;
-        const float start = keeper && kc < p.C && tile < tiles ? p.saved[(b * tiles + tile) * p.C + kc] : 0.f;
+        Lanes<CX> in_h, in_g;
+        read<CX>(in_h, tile < tiles ? p.saved + (b * tiles + tile) * p.C : nullptr, c0 + first, p.C);
         copies_arrived<Rg::STAGES - 1>();
-        const int n = steps_before(len, t0);
         Four a[STEPS], q[STEPS], A, B, H, Q, Ax, Hx, Ay, Qy;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
@@ -303,51 +360,39 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 gate(z.p[j], a[i].p[j], q[i].p[j]);
-                float2 u = mul(q[i].p[j], v.p[j]), e = d.p[j];
-                if (i >= n) { a[i].p[j] = both(1.f); u = e = both(0.f); }
-                if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u; Q.p[j] = mul(A.p[j], e); }
+                const float2 u = mul(q[i].p[j], v.p[j]);
+                if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u; Q.p[j] = mul(A.p[j], d.p[j]); }
                 else {
                     H.p[j] = fma(a[i].p[j], H.p[j], u);
                     A.p[j] = mul(A.p[j], a[i].p[j]);
-                    Q.p[j] = fma(A.p[j], e, Q.p[j]);             // what dy of this step is in front of the thread's first one
+                    Q.p[j] = fma(A.p[j], d.p[j], Q.p[j]);        // what dy of this step is in front of the thread's first one
                 }
             }
         }
         B = A;
         join<CX, true>(A, H, Ax, Hx);                            // of the threads in front (forward map)
         join<CX, false>(B, Q, Ay, Qy);                           // and behind (backward map)
-        if (CX >= 32 || lane >= 32 - CX) { store(&tot_a[team][cx * N], A); store(&tot_h[team][cx * N], H); }
-        if (CX >= 32 || lane < CX) store(&tot_g[team][cx * N], Q);
+        if (CX >= 32 || lane >= 32 - CX) store(&tot_h[now][team][cx * N], A, H);
+        if (CX >= 32 || lane < CX) store(&tot_g[now][team][cx * N], B, Q);
         __syncthreads();
         if (R > 1) {
             cg::cluster_group cl = cg::this_cluster();
-            if (keeper) {
+            if (threadIdx.x < G::CH) {
                 float ta = 1.f, tq = 0.f;
 #pragma unroll
-                for (int w = G::TEAMS - 1; w >= 0; --w) { tq = fmaf(tot_a[w][threadIdx.x], tq, tot_g[w][threadIdx.x]); ta *= tot_a[w][threadIdx.x]; }
-                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[round & 1][rank][threadIdx.x], r) = make_float2(ta, tq);
+                for (int w = G::TEAMS - 1; w >= 0; --w) { const float2 m = tot_g[now][w][threadIdx.x]; tq = fmaf(m.x, tq, m.y); ta *= m.x; }
+                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[now][rank][threadIdx.x], r) = make_float2(ta, tq);
             }
             cl.sync();
-        }
-        if (keeper) {
-            float h = start, g = carry;
-            if (R > 1)
-                for (int r = R - 1; r >= 0; --r) {
-                    const float2 m = joined[round & 1][r][threadIdx.x];
-                    if (r == rank) g = carry;
-                    carry = fmaf(m.x, carry, m.y);
-                }
-#pragma unroll
-            for (int w = 0; w < G::TEAMS; ++w) {
-                const int x = G::TEAMS - 1 - w;
-                in_h[w][threadIdx.x] = h; h = fmaf(tot_a[w][threadIdx.x], h, tot_h[w][threadIdx.x]);
-                in_g[x][threadIdx.x] = g; g = fmaf(tot_a[x][threadIdx.x], g, tot_g[x][threadIdx.x]);
+            for (int r = R - 1; r >= 0; --r) {
+                if (r == rank) in_g = carry;
+                carry.through(&joined[now][r][first]);
             }
-            if (R == 1) carry = g;
-        }
-        __syncthreads();
-        Four g = load(&in_g[team][cx * N]), before[STEPS];
-        before[0] = load(&in_h[team][cx * N]);
+        } else in_g.set(&carried[now][first]);
+        for (int w = 0; w < team; ++w) in_h.through(&tot_h[now][w][first]);
+        for (int w = G::TEAMS - 1; w > team; --w) in_g.through(&tot_g[now][w][first]);
+        Four g = in_g.four(), before[STEPS];
+        before[0] = in_h.four();
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             before[0].p[j] = fma(Ax.p[j], before[0].p[j], Hx.p[j]);
@@ -359,30 +404,48 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
 #pragma unroll
             for (int j = 0; j < 2; ++j) before[i + 1].p[j] = fma(a[i].p[j], before[i].p[j], mul(q[i].p[j], v.p[j]));
         }
-        const int out = left > 0 ? steps_before(p.T, t0) : 0;
-#pragma unroll
-        for (int i = STEPS - 1; i >= 0; --i) {
+        // one step back: its gradients, and g in front of it
+        auto back = [&](int i, Four& oz, Four& ov) {
             const Four v = unpack(*ring.slot(stage, i, 1)), e = unpack(*ring.slot(stage, i, 2));
-            Four oz{}, ov{};
-            if (i < n) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float2 d = __fadd2_rn(e.p[j], g.p[j]);
-                    ov.p[j] = mul(q[i].p[j], d);
-                    oz.p[j] = mul(mul(a[i].p[j], ov.p[j]), fma(v.p[j], both(-1.f), before[i].p[j]));
-                    g.p[j] = mul(a[i].p[j], d);
-                }
+            for (int j = 0; j < 2; ++j) {
+                const float2 d = __fadd2_rn(e.p[j], g.p[j]);
+                ov.p[j] = mul(q[i].p[j], d);
+                g.p[j] = mul(a[i].p[j], d);
+                oz.p[j] = mul(mul(a[i].p[j], ov.p[j]), fma(v.p[j], both(-1.f), before[i].p[j]));
             }
-            if (i < out) {
+        };
+        const int n = left > 0 ? steps_before(len, t0) : 0;
+        if (n == STEPS) {
+#pragma unroll
+            for (int i = STEPS - 1; i >= 0; --i) {
+                Four oz, ov;
+                back(i, oz, ov);
                 put<T, ACC>(dz + i * p.dz_t, oz, left, p.accum);
                 put<T, ACC>(dv + i * p.dv_t, ov, left, p.accum);
             }
+        } else {
+            const int out = left > 0 ? steps_before(p.T, t0) : 0;
+#pragma unroll
+            for (int i = STEPS - 1; i >= 0; --i) {
+                Four oz, ov;
+                back(i, oz, ov);
+                if (i < out) {
+                    put<T, ACC>(dz + i * p.dz_t, i < n ? oz : Four{}, left, p.accum);
+                    put<T, ACC>(dv + i * p.dv_t, i < n ? ov : Four{}, left, p.accum);
+                }
+            }
         }
-        t0 -= stride; dz -= stride * p.dz_t; dv -= stride * p.dv_t;
+        if (R == 1 && tg == 0) *(float4*)&carried[now ^ 1][cx * N] = make_float4(g.p[0].x, g.p[0].y, g.p[1].x, g.p[1].y);
+        t0 -= stride; tile -= R; dz -= stride * p.dz_t; dv -= stride * p.dv_t;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    if (p.dstate && keeper && rank == 0 && kc < p.C) p.dstate[b * p.C + kc] = carry;
     if (R > 1) cg::this_cluster().sync();
+    else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
+    if (p.dstate && rank == 0 && threadIdx.x < G::TEAM) {
+#pragma unroll
+        for (int j = 0; j < Lanes<CX>::M; ++j) if (c0 + first + j < p.C) p.dstate[b * p.C + c0 + first + j] = carry.v[j];
+    }
 }
 
 // How a launch is cut: CX threads along the channels, clusters of R CTAs along the steps.
