@@ -65,7 +65,7 @@ fdg_status embedding_sizes(const char* fn, int64_t n, int64_t vocab, int64_t cha
 fdg_status recurrence_sizes(const char* fn, const fdg_recurrence* s) {
     if (!s) return fail(FDG_ERR_INVALID_ARG, "%s: shape is NULL", fn);
     if (bad_dtype(s->dtype)) return fail(FDG_ERR_INVALID_ARG, "%s: dtype must be 0 (fp32) or 1 (bf16)", fn);
-    if (bad_extent(s->batch) || bad_extent(s->steps) || s->channels < 1 || s->channels > (1 << 20)) return fail(FDG_ERR_INVALID_ARG, "%s: batch and steps must be 0..2^31-1, channels 1..2^20", fn);
+    if (bad_extent(s->batch) || s->steps < 0 || s->steps > (1 << 30) || s->channels < 1 || s->channels > (1 << 20)) return fail(FDG_ERR_INVALID_ARG, "%s: batch must be 0..2^31-1, steps 0..2^30, channels 1..2^20", fn);
     if ((__int128)s->batch * s->steps * s->channels >= (__int128)1 << 46) return fail(FDG_ERR_INVALID_ARG, "%s: the tensors are too large", fn);
     return FDG_OK;
 }

@@ -26,13 +26,13 @@ using bf16 = __nv_bfloat16;
 constexpr int THREADS = 256;
 constexpr int STEPS = 4;                // of a thread in a tile
 constexpr int N = 4;                    // channels of a thread
-constexpr int MAX_CLUSTER = 8;      // of slices up to 64 channels; wider ones have no clusters
+constexpr int MAX_CLUSTER = 8;      // of slices up to 32 channels; wider ones have no clusters
 
 // CX threads lie along the channels, the others along the steps.
 template <int CX> struct Geo {
     static constexpr int TG = THREADS / CX, CH = CX * N, TILE = TG * STEPS;
     static constexpr int TEAM = CX < 32 ? 32 : CX, TEAMS = THREADS / TEAM;      // a team joins its threads by shuffles (or is one step group)
-    static constexpr int RANKS = CX > 16 ? 1 : MAX_CLUSTER;
+    static constexpr int RANKS = CX > 8 ? 1 : MAX_CLUSTER;
 };
 
 // Values go in pairs through the packed fp32 instructions: the kernels issue too much, not too little, to keep up with HBM.
@@ -114,10 +114,7 @@ template <typename T, int ACC> __device__ __forceinline__ void put(T* g, Four x,
     }
 }
 // steps of t0 .. t0 + STEPS - 1 that lie in front of `end`
-__device__ __forceinline__ int steps_before(long end, long t0) {
-    const long n = end - t0;
-    return n <= 0 ? 0 : n < STEPS ? (int)n : STEPS;
-}
+__device__ __forceinline__ int steps_before(int end, int t0) { return min(max(end - t0, 0), STEPS); }
 
 template <typename T, int TENSORS> struct Ring {
     using V = typename Raw<T>::V;
@@ -128,43 +125,23 @@ template <typename T, int TENSORS> struct Ring {
     __device__ V* slot(int stage, int i, int tensor) const { return mine + stage * STAGE + (i * TENSORS + tensor) * THREADS; }
 };
 
-// the map (a1, h1), then (a, h), in place of (a, h)
-__device__ __forceinline__ void after(float2 a1, float2 h1, float2& a, float2& h) { h = fma(a, h1, h); a = mul(a, a1); }
-__device__ __forceinline__ float2 shfl_up(float2 v, int d) { return make_float2(__shfl_up_sync(~0u, v.x, d), __shfl_up_sync(~0u, v.y, d)); }
-__device__ __forceinline__ float2 shfl_down(float2 v, int d) { return make_float2(__shfl_down_sync(~0u, v.x, d), __shfl_down_sync(~0u, v.y, d)); }
-// Over the step groups of a warp: (A, H) becomes the map of the groups up to and with this one, (Ax, Hx) that of those before it; UP: in the order of
-// the lanes, else against it.
-template <int CX, bool UP> __device__ __forceinline__ void join(Four& A, Four& H, Four& Ax, Four& Hx) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) { Ax.p[j] = both(1.f); Hx.p[j] = both(0.f); }
-#pragma unroll
-    for (int d = CX; d < 32; d *= 2)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float2 a = UP ? shfl_up(A.p[j], d) : shfl_down(A.p[j], d), h = UP ? shfl_up(H.p[j], d) : shfl_down(H.p[j], d);
-            if (UP ? lane >= d : lane < 32 - d) {
-                after(a, h, A.p[j], H.p[j]);
-                if (d == CX) { Ax.p[j] = a; Hx.p[j] = h; } else after(a, h, Ax.p[j], Hx.p[j]);
-            }
-        }
-}
-// Maps of the teams, one {A, H} per channel.
-__device__ __forceinline__ void store(float2* p, const Four& A, const Four& H) {
-    *(float4*)p = make_float4(A.p[0].x, H.p[0].x, A.p[0].y, H.p[0].y);
-    *(float4*)(p + 2) = make_float4(A.p[1].x, H.p[1].x, A.p[1].y, H.p[1].y);
-}
-// The value that stands in front of a warp, for the channels of its lanes, from values and maps per channel.  Up to 32 channels a lane takes one channel
-// through the maps and the lanes exchange them; above, every lane takes its own four.
-template <int CX> struct Lanes {
-    static constexpr bool ONE = CX * N <= 32;
-    static constexpr int M = ONE ? 1 : N;
+__device__ __forceinline__ void store(float* p, const Four& x) { *(float4*)p = make_float4(x.p[0].x, x.p[0].y, x.p[1].x, x.p[1].y); }
+__device__ __forceinline__ Four load(const float* p) { const float4 r = *(const float4*)p; return {make_float2(r.x, r.y), make_float2(r.z, r.w)}; }
+
+// Joining the maps of a tile.  Up to 32 channels (CX <= 8) a warp holds several step groups: its threads leave their maps in shared memory, and a lane takes one channel
+// and LINKS = 4 of the groups from there; above (a team is one step group) a lane has its own four channels.
+template <int CX> struct Lane {
+    static constexpr bool ONE = CX <= 8;
+    static constexpr int M = ONE ? 1 : N, CH = CX * N, LINKS = 4, SUBS = ONE ? 32 / CX / LINKS : 1;
+    static __device__ __forceinline__ int first() { return ONE ? (threadIdx.x & 31) % CH : threadIdx.x % CX * N; }      // channel of the slice
+    static __device__ __forceinline__ int sub() { return ONE ? (threadIdx.x & 31) / CH : 0; }
+    static __device__ __forceinline__ bool writes() { return ONE ? (threadIdx.x & 31) < CH : true; }
     float v[M];
-    static __device__ __forceinline__ int first() { return ONE ? (threadIdx.x & 31) % (CX * N) : threadIdx.x % CX * N; }
     __device__ __forceinline__ void set(const float* p) {
         if constexpr (ONE) v[0] = *p;
         else { const float4 r = *(const float4*)p; v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
     }
+    // through the map at p: {A, H} of each channel
     __device__ __forceinline__ void through(const float2* p) {
         if constexpr (ONE) { const float2 m = *p; v[0] = fmaf(m.x, v[0], m.y); }
         else {
@@ -172,42 +149,75 @@ template <int CX> struct Lanes {
             v[0] = fmaf(m.x, v[0], m.y); v[1] = fmaf(m.z, v[1], m.w); v[2] = fmaf(k.x, v[2], k.y); v[3] = fmaf(k.z, v[3], k.w);
         }
     }
-    __device__ __forceinline__ Four four() const {
-        if constexpr (ONE) {
-            const int l = threadIdx.x % CX * N;
-            return {make_float2(__shfl_sync(~0u, v[0], l), __shfl_sync(~0u, v[0], l + 1)), make_float2(__shfl_sync(~0u, v[0], l + 2), __shfl_sync(~0u, v[0], l + 3))};
-        } else return {make_float2(v[0], v[1]), make_float2(v[2], v[3])};
+    // values of a row of C channels, c0: the slice's first
+    __device__ __forceinline__ void read(const float* row, long c0, long C) {
+#pragma unroll
+        for (int j = 0; j < M; ++j) v[j] = row && c0 + first() + j < C ? row[c0 + first() + j] : 0.f;
+    }
+    __device__ __forceinline__ void write(float* row, long c0, long C) const {
+#pragma unroll
+        for (int j = 0; j < M; ++j) if (c0 + first() + j < C) row[c0 + first() + j] = v[j];
     }
 };
-// values of channels first .. of a row of C, zero behind its end
-template <int CX> __device__ __forceinline__ void read(Lanes<CX>& l, const float* row, long first, long C) {
+// The maps of a warp's step groups, in order (UP) or against it.
+template <int CX, bool UP> struct Chain {
+    using L = Lane<CX>;
+    float a[L::LINKS], h[L::LINKS], ta, th;         // of the lane's groups; of all the warp's
+    float fa, fh;                                   // of the groups of the lanes before this one's
+    static __device__ __forceinline__ int at(int k) { return (L::sub() * L::LINKS + (UP ? k : L::LINKS - 1 - k)) * L::CH + L::first(); }
+    // wa, wh: [step group][channel] of this warp
+    __device__ __forceinline__ void read(const float* wa, const float* wh) {
 #pragma unroll
-    for (int j = 0; j < Lanes<CX>::M; ++j) l.v[j] = row && first + j < C ? row[first + j] : 0.f;
+        for (int k = 0; k < L::LINKS; ++k) { a[k] = wa[at(k)]; h[k] = wh[at(k)]; }
+        ta = a[0]; th = h[0];
+#pragma unroll
+        for (int k = 1; k < L::LINKS; ++k) { th = fmaf(a[k], th, h[k]); ta *= a[k]; }
+        fa = 1.f; fh = 0.f;
+        if constexpr (L::SUBS == 2) {
+            const float oa = __shfl_xor_sync(~0u, ta, L::CH), oh = __shfl_xor_sync(~0u, th, L::CH);
+            const bool later = (L::sub() == 1) == UP;
+            if (later) { fa = oa; fh = oh; th = fmaf(ta, oh, th); } else th = fmaf(oa, th, oh);
+            ta *= oa;
+        }
+    }
+    // from the value in front of the warp: the values in front of its groups, to w (may be wh)
+    __device__ __forceinline__ void apply(float v, float* w) const {
+        v = fmaf(fa, v, fh);
+#pragma unroll
+        for (int k = 0; k < L::LINKS; ++k) { w[at(k)] = v; v = fmaf(a[k], v, h[k]); }
+    }
+};
+__device__ __forceinline__ void store(float2* p, const Four& A, const Four& H) {
+    *(float4*)p = make_float4(A.p[0].x, H.p[0].x, A.p[0].y, H.p[0].y);
+    *(float4*)(p + 2) = make_float4(A.p[1].x, H.p[1].x, A.p[1].y, H.p[1].y);
 }
 
 // One barrier a tile: behind it a warp goes through the maps of the teams in front of it by itself, and the last steps' threads leave the state for the
 // next tile, which the next tile's barrier orders.  What stands there is kept twice, by the round's parity.
-template <typename T, int ACC, int CX>
-__global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, int slices) {
+template <typename T, int ACC, int CX, bool CLUSTER>
+__global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int ranks, int slices) {
+    const int R = CLUSTER ? ranks : 1;
     using G = Geo<CX>;
     using Rg = Ring<T, 2>;
     extern __shared__ __align__(16) char dyn[];
     const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
     __shared__ __align__(16) float2 tot[2][G::TEAMS][G::CH];
+    __shared__ __align__(16) float own[2][Lane<CX>::ONE ? THREADS * N : 1];      // a warp's maps, later the states in front of its step groups
     __shared__ __align__(16) float carried[2][G::CH];
     __shared__ __align__(16) float2 joined[2][G::RANKS][G::CH];
-    const int rank = R > 1 ? (int)(blockIdx.x % R) : 0;
+    const int rank = CLUSTER ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
-    const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM, lane = threadIdx.x & 31;
+    const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM;
     const long c = c0 + cx * N;
     const int left = (int)min((long)N, p.C - c);                 // channels of this thread that exist
-    const long len = p.lengths ? min((long)max(p.lengths[b], 0), p.T) : p.T;
-    const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = (long)R * G::TILE;
-    long t0 = (long)rank * G::TILE + tg * STEPS, tf = t0;        // this thread's first step: of the round, of the next tile to fetch
+    const int T_ = (int)p.T, len = p.lengths ? min(max(p.lengths[b], 0), T_) : T_;
+    const int tiles = (T_ + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = R * G::TILE;
+    int t0 = rank * G::TILE + tg * STEPS, tf = t0;        // this thread's first step: of the round, of the next tile to fetch
     const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
     const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
     T* y = (T*)p.y + b * p.y_b + c + t0 * p.y_t;
+    const long z_round = stride * p.z_t, v_round = stride * p.v_t, y_round = stride * p.y_t;
     auto fetch_tile = [&](int stage) {
         const int n = left > 0 ? steps_before(len, tf) : 0;
 #pragma unroll
@@ -217,21 +227,21 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
                 fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
             } else idle(ring.slot(stage, i, 0), ring.slot(stage, i, 1));
         copies_issued();
-        tf += stride; zf += stride * p.z_t; vf += stride * p.v_t;
+        tf += stride; zf += z_round; vf += v_round;
     };
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
-    if (R > 1) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
-    const int first = Lanes<CX>::first();
-    Lanes<CX> carry;                                             // R > 1: the state in front of the round, in every warp
-    read<CX>(carry, p.state ? p.state + b * p.C : nullptr, c0 + first, p.C);
+    if (CLUSTER) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
+    const int first = Lane<CX>::first(), mine = (threadIdx.x & ~31) * N;
+    Lane<CX> carry;                                              // CLUSTER: the state in front of the round, in every warp
+    carry.read(p.state ? p.state + b * p.C : nullptr, c0, p.C);
     if (threadIdx.x < G::CH) carried[0][threadIdx.x] = p.state && c0 + threadIdx.x < p.C ? p.state[b * p.C + c0 + threadIdx.x] : 0.f;
     int stage = 0;
-    for (long round = 0; round < rounds; ++round) {
-        const int now = (int)(round & 1);
+    for (int round = 0; round < rounds; ++round) {
+        const int now = round & 1;
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
         copies_arrived<Rg::STAGES - 1>();
         // the map of this thread's steps
-        Four a[STEPS], u[STEPS], A, H, Ax, Hx;
+        Four a[STEPS], u[STEPS], A, H;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const Four z = unpack(*ring.slot(stage, i, 0)), v = unpack(*ring.slot(stage, i, 1));
@@ -244,11 +254,17 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
                 else { H.p[j] = fma(a[i].p[j], H.p[j], u[i].p[j]); A.p[j] = mul(A.p[j], a[i].p[j]); }
             }
         }
-        join<CX, true>(A, H, Ax, Hx);                            // of the threads in front of it in its team, and the team's
-        if (CX >= 32 || lane >= 32 - CX) store(&tot[now][team][cx * N], A, H);
+        Chain<CX, true> chain;
+        if constexpr (Lane<CX>::ONE) {
+            __syncwarp();
+            store(&own[0][threadIdx.x * N], A); store(&own[1][threadIdx.x * N], H);
+            __syncwarp();
+            chain.read(&own[0][mine], &own[1][mine]);
+            if (Lane<CX>::writes()) tot[now][team][first] = make_float2(chain.ta, chain.th);
+        } else store(&tot[now][team][first], A, H);
         __syncthreads();
-        Lanes<CX> in;
-        if (R > 1) {                                             // the CTA's map goes to every CTA of the cluster
+        Lane<CX> in;
+        if (CLUSTER) {                                             // the CTA's map goes to every CTA of the cluster
             cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < G::CH) {
                 float ta = 1.f, th = 0.f;
@@ -262,15 +278,14 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
                 carry.through(&joined[now][r][first]);
             }
         } else in.set(&carried[now][first]);
-        if (p.saved && threadIdx.x < G::TEAM && (!Lanes<CX>::ONE || lane < G::CH) && (Lanes<CX>::ONE || CX >= 32 || lane < CX)) {
-            const long tile = round * R + rank;
-#pragma unroll
-            for (int j = 0; j < Lanes<CX>::M; ++j) if (tile < tiles && c0 + first + j < p.C) p.saved[(b * tiles + tile) * p.C + c0 + first + j] = in.v[j];
-        }
+        if (p.saved && threadIdx.x < G::TEAM && Lane<CX>::writes() && round * R + rank < tiles) in.write(p.saved + ((long)b * tiles + round * R + rank) * p.C, c0, p.C);
         for (int w = 0; w < team; ++w) in.through(&tot[now][w][first]);
-        Four h = in.four();
-#pragma unroll
-        for (int j = 0; j < 2; ++j) h.p[j] = fma(Ax.p[j], h.p[j], Hx.p[j]);
+        Four h;
+        if constexpr (Lane<CX>::ONE) {
+            chain.apply(in.v[0], &own[1][mine]);
+            __syncwarp();
+            h = load(&own[1][threadIdx.x * N]);
+        } else h = {make_float2(in.v[0], in.v[1]), make_float2(in.v[2], in.v[3])};
         const int n = left > 0 ? steps_before(len, t0) : 0;
         if (n == STEPS) {
 #pragma unroll
@@ -280,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
                 put<T, ACC>(y + i * p.y_t, h, left, false);
             }
         } else {
-            const int out = left > 0 ? steps_before(p.T, t0) : 0;
+            const int out = left > 0 ? steps_before(T_, t0) : 0;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
 #pragma unroll
@@ -288,43 +303,42 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int R, in
                 if (i < out) put<T, ACC>(y + i * p.y_t, i < n ? h : Four{}, left, false);
             }
         }
-        if (R == 1 && tg == G::TG - 1) *(float4*)&carried[now ^ 1][cx * N] = make_float4(h.p[0].x, h.p[0].y, h.p[1].x, h.p[1].y);
-        t0 += stride; y += stride * p.y_t;
+        if (!CLUSTER && tg == G::TG - 1) *(float4*)&carried[now ^ 1][cx * N] = make_float4(h.p[0].x, h.p[0].y, h.p[1].x, h.p[1].y);
+        t0 += stride; y += y_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    if (R > 1) cg::this_cluster().sync();                        // nobody leaves while others may write to its shared memory
+    if (CLUSTER) cg::this_cluster().sync();                        // nobody leaves while others may write to its shared memory
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
-    if (p.state_out && rank == 0 && threadIdx.x < G::TEAM) {
-#pragma unroll
-        for (int j = 0; j < Lanes<CX>::M; ++j) if (c0 + first + j < p.C) p.state_out[b * p.C + c0 + first + j] = carry.v[j];
-    }
+    if (p.state_out && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.state_out + b * p.C, c0, p.C);
 }
 
-template <typename T, int ACC, int CX>
-__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, int slices) {
+template <typename T, int ACC, int CX, bool CLUSTER>
+__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks, int slices) {
+    const int R = CLUSTER ? ranks : 1;
     using G = Geo<CX>;
     using Rg = Ring<T, 3>;
     extern __shared__ __align__(16) char dyn[];
     const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
     __shared__ __align__(16) float2 tot_h[2][G::TEAMS][G::CH], tot_g[2][G::TEAMS][G::CH];
+    __shared__ __align__(16) float own[3][Lane<CX>::ONE ? THREADS * N : 1];
     __shared__ __align__(16) float carried[2][G::CH];
     __shared__ __align__(16) float2 joined[2][G::RANKS][G::CH];
-    const int rank = R > 1 ? (int)(blockIdx.x % R) : 0;
+    const int rank = CLUSTER ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
-    const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM, lane = threadIdx.x & 31;
+    const int cx = threadIdx.x % CX, tg = threadIdx.x / CX, team = threadIdx.x / G::TEAM;
     const long c = c0 + cx * N;
     const int left = (int)min((long)N, p.C - c);
-    const long len = p.lengths ? min((long)max(p.lengths[b], 0), p.T) : p.T;
-    const long tiles = (p.T + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = (long)R * G::TILE;
+    const int T_ = (int)p.T, len = p.lengths ? min(max(p.lengths[b], 0), T_) : T_;
+    const int tiles = (T_ + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = R * G::TILE;
     // rounds go from the end of the sequence to its beginning
-    long tile = (rounds - 1) * R + rank;
-    long t0 = tile * G::TILE + tg * STEPS, tf = t0;
+    int tile = (rounds - 1) * R + rank, t0 = tile * G::TILE + tg * STEPS, tf = t0;
     const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
     const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
     const T* df = (const T*)p.dy + b * p.dy_b + c + t0 * p.dy_t;
     T* dz = (T*)p.dz + b * p.dz_b + c + t0 * p.dz_t;
     T* dv = (T*)p.dv + b * p.dv_b + c + t0 * p.dv_t;
+    const long z_round = stride * p.z_t, v_round = stride * p.v_t, d_round = stride * p.dy_t, dz_round = stride * p.dz_t, dv_round = stride * p.dv_t;
     auto fetch_tile = [&](int stage) {
         const int n = left > 0 && tf >= 0 ? steps_before(len, tf) : 0;
 #pragma unroll
@@ -338,22 +352,22 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
                 *ring.slot(stage, i, 2) = *ring.slot(stage, i, 1);
             }
         copies_issued();
-        tf -= stride; zf -= stride * p.z_t; vf -= stride * p.v_t; df -= stride * p.dy_t;
+        tf -= stride; zf -= z_round; vf -= v_round; df -= d_round;
     };
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
-    if (R > 1) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
-    const int first = Lanes<CX>::first();
-    Lanes<CX> carry;
-    read<CX>(carry, p.dstate_out ? p.dstate_out + b * p.C : nullptr, c0 + first, p.C);
+    if (CLUSTER) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
+    const int first = Lane<CX>::first(), mine = (threadIdx.x & ~31) * N;
+    Lane<CX> carry;
+    carry.read(p.dstate_out ? p.dstate_out + b * p.C : nullptr, c0, p.C);
     if (threadIdx.x < G::CH) carried[0][threadIdx.x] = p.dstate_out && c0 + threadIdx.x < p.C ? p.dstate_out[b * p.C + c0 + threadIdx.x] : 0.f;
     int stage = 0;
-    for (long round = 0; round < rounds; ++round) {
-        const int now = (int)(round & 1);
+    for (int round = 0; round < rounds; ++round) {
+        const int now = round & 1;
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
-        Lanes<CX> in_h, in_g;
-        read<CX>(in_h, tile < tiles ? p.saved + (b * tiles + tile) * p.C : nullptr, c0 + first, p.C);
+        Lane<CX> in_h, in_g;
+        in_h.read(tile < tiles ? p.saved + ((long)b * tiles + tile) * p.C : nullptr, c0, p.C);
         copies_arrived<Rg::STAGES - 1>();
-        Four a[STEPS], q[STEPS], A, B, H, Q, Ax, Hx, Ay, Qy;
+        Four a[STEPS], q[STEPS], A, H, Q;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const Four z = unpack(*ring.slot(stage, i, 0)), v = unpack(*ring.slot(stage, i, 1)), d = unpack(*ring.slot(stage, i, 2));
@@ -369,13 +383,21 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
                 }
             }
         }
-        B = A;
-        join<CX, true>(A, H, Ax, Hx);                            // of the threads in front (forward map)
-        join<CX, false>(B, Q, Ay, Qy);                           // and behind (backward map)
-        if (CX >= 32 || lane >= 32 - CX) store(&tot_h[now][team][cx * N], A, H);
-        if (CX >= 32 || lane < CX) store(&tot_g[now][team][cx * N], B, Q);
+        Chain<CX, true> front;                                   // the forward map
+        Chain<CX, false> behind;                                 // the backward map
+        if constexpr (Lane<CX>::ONE) {
+            __syncwarp();
+            store(&own[0][threadIdx.x * N], A); store(&own[1][threadIdx.x * N], H); store(&own[2][threadIdx.x * N], Q);
+            __syncwarp();
+            front.read(&own[0][mine], &own[1][mine]);
+            behind.read(&own[0][mine], &own[2][mine]);
+            if (Lane<CX>::writes()) {
+                tot_h[now][team][first] = make_float2(front.ta, front.th);
+                tot_g[now][team][first] = make_float2(behind.ta, behind.th);
+            }
+        } else { store(&tot_h[now][team][first], A, H); store(&tot_g[now][team][first], A, Q); }
         __syncthreads();
-        if (R > 1) {
+        if (CLUSTER) {
             cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < G::CH) {
                 float ta = 1.f, tq = 0.f;
@@ -391,12 +413,16 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
         } else in_g.set(&carried[now][first]);
         for (int w = 0; w < team; ++w) in_h.through(&tot_h[now][w][first]);
         for (int w = G::TEAMS - 1; w > team; --w) in_g.through(&tot_g[now][w][first]);
-        Four g = in_g.four(), before[STEPS];
-        before[0] = in_h.four();
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            before[0].p[j] = fma(Ax.p[j], before[0].p[j], Hx.p[j]);
-            g.p[j] = fma(Ay.p[j], g.p[j], Qy.p[j]);
+        Four g, before[STEPS];
+        if constexpr (Lane<CX>::ONE) {
+            front.apply(in_h.v[0], &own[1][mine]);
+            behind.apply(in_g.v[0], &own[2][mine]);
+            __syncwarp();
+            before[0] = load(&own[1][threadIdx.x * N]);
+            g = load(&own[2][threadIdx.x * N]);
+        } else {
+            before[0] = {make_float2(in_h.v[0], in_h.v[1]), make_float2(in_h.v[2], in_h.v[3])};
+            g = {make_float2(in_g.v[0], in_g.v[1]), make_float2(in_g.v[2], in_g.v[3])};
         }
 #pragma unroll
         for (int i = 0; i + 1 < STEPS; ++i) {
@@ -425,7 +451,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
                 put<T, ACC>(dv + i * p.dv_t, ov, left, p.accum);
             }
         } else {
-            const int out = left > 0 ? steps_before(p.T, t0) : 0;
+            const int out = left > 0 ? steps_before(T_, t0) : 0;
 #pragma unroll
             for (int i = STEPS - 1; i >= 0; --i) {
                 Four oz, ov;
@@ -436,16 +462,13 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int R, in
                 }
             }
         }
-        if (R == 1 && tg == 0) *(float4*)&carried[now ^ 1][cx * N] = make_float4(g.p[0].x, g.p[0].y, g.p[1].x, g.p[1].y);
-        t0 -= stride; tile -= R; dz -= stride * p.dz_t; dv -= stride * p.dv_t;
+        if (!CLUSTER && tg == 0) *(float4*)&carried[now ^ 1][cx * N] = make_float4(g.p[0].x, g.p[0].y, g.p[1].x, g.p[1].y);
+        t0 -= stride; tile -= R; dz -= dz_round; dv -= dv_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    if (R > 1) cg::this_cluster().sync();
+    if (CLUSTER) cg::this_cluster().sync();
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
-    if (p.dstate && rank == 0 && threadIdx.x < G::TEAM) {
-#pragma unroll
-        for (int j = 0; j < Lanes<CX>::M; ++j) if (c0 + first + j < p.C) p.dstate[b * p.C + c0 + first + j] = carry.v[j];
-    }
+    if (p.dstate && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.dstate + b * p.C, c0, p.C);
 }
 
 // How a launch is cut: CX threads along the channels, clusters of R CTAs along the steps.
@@ -462,31 +485,30 @@ Cut cut(long B, long T, long C) {
     Cut k{64, 1};
     const char* e = getenv("RCX");      // probe
     if (e) { k.cx = atoi(e); k.r = atoi(getenv("RR")); return k; }
-    while (k.cx > 4 && T > tile(k.cx) && B * ((C + 4 * k.cx - 1) / (4 * k.cx)) < 3 * 148) k.cx /= 4;
+    while (k.cx > 4 && T > tile(k.cx) && B * ((C + 4 * k.cx - 1) / (4 * k.cx)) < 3 * 148) k.cx = k.cx == 32 ? 8 : k.cx / 2;
     const long ctas = B * ((C + 4 * k.cx - 1) / (4 * k.cx)), tiles = (T + tile(k.cx) - 1) / tile(k.cx);
-    while (k.r < MAX_CLUSTER && ctas * k.r < 2 * 148 && tiles > k.r) k.r *= 2;
+    while (k.cx <= 8 && k.r < MAX_CLUSTER && ctas * k.r < 2 * 148 && tiles > k.r) k.r *= 2;
     return k;
 }
 
-template <typename T, int ACC, int CX, bool BACK>
+template <typename T, int ACC, int CX, bool BACK, bool CLUSTER>
 cudaError_t launch(const RecurArgs& a, int R, cudaStream_t s) {
     constexpr int bytes = BACK ? Ring<T, 3>::BYTES : Ring<T, 2>::BYTES;
     static OncePerDevice once;
-    const auto k = BACK ? recur_bwd_k<T, ACC, CX> : recur_fwd_k<T, ACC, CX>;
+    const auto k = BACK ? recur_bwd_k<T, ACC, CX, CLUSTER> : recur_fwd_k<T, ACC, CX, CLUSTER>;
     const cudaError_t e = allow_smem(once, (const void*)k, bytes);
     if (e != cudaSuccess) return e;
     const int slices = (int)((a.C + Geo<CX>::CH - 1) / Geo<CX>::CH);
-    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, bytes, s, R > 1 ? R : 0, a, R, slices);
+    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, bytes, s, CLUSTER ? R : 0, a, R, slices);
 }
 template <typename T, int ACC, bool BACK>
 cudaError_t pick(const RecurArgs& a, cudaStream_t s) {
     const Cut k = cut(a.B, a.T, a.C);
     switch (k.cx) {
-        case 4: return launch<T, ACC, 4, BACK>(a, k.r, s);
-        case 8: return launch<T, ACC, 8, BACK>(a, k.r, s);
-        case 16: return launch<T, ACC, 16, BACK>(a, k.r, s);
-        case 32: return launch<T, ACC, 32, BACK>(a, k.r, s);
-        default: return launch<T, ACC, 64, BACK>(a, k.r, s);
+        case 4: return k.r > 1 ? launch<T, ACC, 4, BACK, true>(a, k.r, s) : launch<T, ACC, 4, BACK, false>(a, 1, s);
+        case 8: return k.r > 1 ? launch<T, ACC, 8, BACK, true>(a, k.r, s) : launch<T, ACC, 8, BACK, false>(a, 1, s);
+        case 32: return launch<T, ACC, 32, BACK, false>(a, 1, s);
+        default: return launch<T, ACC, 64, BACK, false>(a, 1, s);
     }
 }
 // elements (4, 2, 1) that may be moved at once: every row of every tensor starts on that many
