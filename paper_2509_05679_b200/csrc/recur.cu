@@ -15,7 +15,6 @@
 
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
-#include <cstdlib>
 
 namespace fdg {
 namespace {
@@ -471,23 +470,17 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
     if (p.dstate && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.dstate + b * p.C, c0, p.C);
 }
 
-// How a launch is cut: CX threads along the channels, clusters of R CTAs along the steps.
+// How a launch is cut: cx threads along the channels, clusters of r CTAs along the steps.  Both directions use the same cut (the states in front of the tiles
+// pass between them), and it depends on the sizes alone.
 struct Cut { int cx, r; };
-int sms() {
-    static int n[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
-    if (!n[dev]) { int v = 0; cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev); n[dev] = v > 0 ? v : 148; }
-    return n[dev];
-}
 Cut cut(long B, long T, long C) {
-    auto tile = [](int cx) { return THREADS / cx * STEPS; };
-    Cut k{64, 1};
-    const char* e = getenv("RCX");      // probe
-    if (e) { k.cx = atoi(e); k.r = atoi(getenv("RR")); return k; }
-    while (k.cx > 4 && T > tile(k.cx) && B * ((C + 4 * k.cx - 1) / (4 * k.cx)) < 3 * 148) k.cx = k.cx == 32 ? 8 : k.cx / 2;
-    const long ctas = B * ((C + 4 * k.cx - 1) / (4 * k.cx)), tiles = (T + tile(k.cx) - 1) / tile(k.cx);
-    while (k.cx <= 8 && k.r < MAX_CLUSTER && ctas * k.r < 2 * 148 && tiles > k.r) k.r *= 2;
+    if (T <= 16) return {64, 1};
+    if (T <= 32) return {32, 1};
+    auto tiles = [&](int cx) { return (T + THREADS / cx * STEPS - 1) / (THREADS / cx * STEPS); };
+    auto ctas = [&](int cx) { return B * ((C + N * cx - 1) / (N * cx)); };
+    Cut k{8, 1};
+    if (ctas(8) * MAX_CLUSTER < 2 * 148) k.cx = 4;
+    while (k.r < MAX_CLUSTER && ctas(k.cx) * k.r * 2 <= 2 * 148 && tiles(k.cx) >= 16 * k.r) k.r *= 2;
     return k;
 }
 
