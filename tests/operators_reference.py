@@ -109,7 +109,9 @@ def recurrence_grad(gate, value, state, lengths, dy, dstate):
 
 def distill(logits, labels, ids, teacher, tau, weight, scale, grad_dtype):
     """((loss, bound), (gradient, bound)).  An exponential of x = (s - max) / tau is off by (3 |x| + 4) U relative (difference, product, the function), a sum over the
-    vocabulary in at least 256 parts by `depth` U more, a logarithm of it by as much absolutely."""
+    vocabulary in at least 256 parts by `depth` U more, a logarithm of it by as much absolutely.  An exponential below TINY, the least normal number, may count as
+    zero (it is one of a sum that is at least 1, the maximum's own): that takes at most TINY from q, V TINY from the sum, which is nothing beside U."""
+    TINY = 2.0 ** -126
     m, v = logits.shape
     x = logits.to(F64)
     live = torch.ones(m, dtype=torch.bool, device=logits.device) if labels is None else (labels >= 0) & (labels < v)
@@ -148,7 +150,7 @@ def distill(logits, labels, ids, teacher, tau, weight, scale, grad_dtype):
         serr = torch.zeros_like(x).scatter_add_(1, at, torch.where(inside, p * (perr + ids.shape[1] * U), 0.0))
         on = taught.to(F64) * weight * tau
         grad = on * (q - soft)
-        gerr = on * (q * qrel + serr + 4 * U * (q + soft))
+        gerr = on * (q * qrel + serr + 4 * U * (q + soft) + TINY)
     if weight < 1:
         q, lq, qrel, lqabs = softmax(1.0)
         one = torch.zeros_like(x).scatter_(1, y[:, None], 1.0)
@@ -156,7 +158,7 @@ def distill(logits, labels, ids, teacher, tau, weight, scale, grad_dtype):
         loss = loss + (1 - weight) * hard
         lerr = lerr + (1 - weight) * (lqabs.gather(1, y[:, None])[:, 0] + 2 * U * hard.abs())
         grad = grad + (1 - weight) * (q - one)
-        gerr = gerr + (1 - weight) * (q * qrel + 4 * U * (q + one))
+        gerr = gerr + (1 - weight) * (q * qrel + 4 * U * (q + one) + TINY)
     lerr = lerr + 4 * U * loss.abs()
     gerr = gerr + 2 * U * grad.abs()
     live2 = live[:, None]
