@@ -58,7 +58,7 @@ bool bad_dtype(int32_t d) { return d != 0 && d != 1; }
 bool bad_extent(int64_t v) { return v < 0 || v >= MOST; }
 
 fdg_status embedding_sizes(const char* fn, int64_t n, int64_t vocab, int64_t channels) {
-    if (bad_extent(n) || vocab < 1 || vocab >= MOST - 1 || channels < 1 || channels > (1 << 20)) return fail(FDG_ERR_INVALID_ARG, "%s: n must be 0..2^31-1, vocab 1..2^31-2, channels 1..2^20", fn);
+    if (n < 0 || n > (1 << 30) || vocab < 1 || vocab >= MOST - 1 || channels < 1 || channels > (1 << 20)) return fail(FDG_ERR_INVALID_ARG, "%s: n must be 0..2^30, vocab 1..2^31-2, channels 1..2^20", fn);
     return FDG_OK;
 }
 
