@@ -4,14 +4,15 @@
 //
 // The gradient's sums are made in the order of the tokens' positions (in pieces of fixed size), never by atomic additions, so that equal inputs give equal bits.
 // Few tokens: a warp per token looks through all of them.  Otherwise the positions are sorted by token (stable) and the sorted list is cut into tiles:
-//   sort    one cluster of CTAs, a radix sort of 8 or 9 bits a pass through L2, while the other SMs fill the table's gradient with zeros
+//   sort    every CTA owns a range of the table's rows: it picks the tokens of its range out of all (and counts the smaller ones, so it knows its place in the
+//           list without asking anyone), sorts them, and fills the rows that none names with zeros.  Reading all tokens in every CTA costs 1 us per 8000;
+//           a cluster that sorted for all took 56 us for 131072 tokens beside SMs that waited
 //   sums    a team of threads per tile adds the rows up, and writes a token's sum when the next one begins; a sum that began in an earlier tile is left as
 //           a partial row
 //   joins   the team of the tile in which a token began adds the partial rows of the following tiles to its row
 #include "seqops.h"
 #include "launch.h"
 
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -19,7 +20,6 @@
 namespace fdg {
 namespace {
 
-namespace cg = cooperative_groups;
 using bf16 = __nv_bfloat16;
 
 // ---- vectors of N values
@@ -73,54 +73,65 @@ __global__ void __launch_bounds__(256) embed_fwd_k(const int32_t* __restrict__ t
     }
 }
 
-// ---- gradient of few tokens, in one launch
-constexpr long FEW = 512;
-constexpr int FILL_ROWS = 4096;                 // rows of the table that a filling CTA looks at a time
-// zeros to elements [lo, hi) of p by the CTA; p on 4 bytes
-__device__ __forceinline__ void zero(float* p, long lo, long hi) {
-    const long a = min(hi, lo + (long)((16 - (uintptr_t)(p + lo) % 16) % 16 / 4)), b = a + (hi - a) / 4 * 4;
-    for (long i = lo + threadIdx.x; i < a; i += blockDim.x) p[i] = 0.f;
-    for (long i = a + 4 * (long)threadIdx.x; i < b; i += 4 * (long)blockDim.x) *(float4*)(p + i) = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (long i = b + threadIdx.x; i < hi; i += blockDim.x) p[i] = 0.f;
+// Zeros to the rows [r0, r1) of dtable that none of n tokens names, by a CTA of THREADS.  Written rows are the bound, so those that the sums write are left
+// out: the CTA marks the rows of its range that occur.
+constexpr int FILL_ROWS = 8192;                 // that it looks at a time
+template <int THREADS, typename Tokens>
+__device__ __forceinline__ void fill_rows(Tokens token, int n, float* dtable, long r0, long r1, int C, bool vec, unsigned* named) {
+    for (long b = r0; b < r1; b += FILL_ROWS) {
+        const int rows = (int)min((long)FILL_ROWS, r1 - b);
+        __syncthreads();
+        for (int i = threadIdx.x; i < (rows + 31) / 32; i += THREADS) named[i] = 0;
+        __syncthreads();
+#pragma unroll 8
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+            const long t = token(i) - b;                        // (common tokens: one atomic operation, not thousands at one address)
+            if (t >= 0 && t < rows && !(((volatile unsigned*)named)[t >> 5] >> (t & 31) & 1)) atomicOr(&named[t >> 5], 1u << (t & 31));
+        }
+        __syncthreads();
+        const unsigned per = vec ? C / 4 : C;
+        float* d = dtable + b * C;
+        unsigned row = threadIdx.x / per, col = threadIdx.x - row * per;
+        const unsigned row_step = THREADS / per, col_step = THREADS - row_step * per;
+        d += (long)threadIdx.x * (vec ? 4 : 1);
+#pragma unroll 4
+        for (; row < (unsigned)rows;) {
+            if (!(named[row >> 5] >> (row & 31) & 1)) { if (vec) *(float4*)d = make_float4(0.f, 0.f, 0.f, 0.f); else *d = 0.f; }
+            d += THREADS * (vec ? 4 : 1);
+            row += row_step; col += col_step;
+            if (col >= per) { col -= per; ++row; }
+        }
+    }
 }
-// CTAs 0 .. warps / 8 - 1: a warp per token and 32 N channels; it goes on if no earlier token is the same, and adds up all that are, in order.  The
+
+// ---- gradient of few tokens, in one launch
+constexpr int FEW = 512;
+// CTAs 0 .. sum_ctas - 1: a warp per token and 32 N channels; it goes on if no earlier token is the same, and adds up all that are, in order.  The
 // others fill the rows that no token names.
 template <typename T, int N>
 __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ tokens, int n, const T* __restrict__ dy, long dys, long vocab, int C, int slices, float scale,
                                                    int accum, float* __restrict__ dtable, int sum_ctas) {
+    __shared__ int tok_[FEW];
+    __shared__ unsigned named[FILL_ROWS / 32];
+#pragma unroll
+    for (int i = 0; i < FEW; i += 256) if (i + threadIdx.x < n) tok_[i + threadIdx.x] = tokens[i + threadIdx.x];
+    __syncthreads();
     if ((int)blockIdx.x >= sum_ctas) {
-        __shared__ unsigned named[FILL_ROWS / 32];
-        const long ctas = gridDim.x - sum_ctas, per = (vocab + ctas - 1) / ctas, r0 = (blockIdx.x - sum_ctas) * per, r1 = min(vocab, r0 + per);
-        for (long b = r0; b < r1; b += FILL_ROWS) {
-            const int rows = (int)min((long)FILL_ROWS, r1 - b);
-            __syncthreads();
-            for (int i = threadIdx.x; i < FILL_ROWS / 32; i += 256) named[i] = 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < n; i += 256) { const long t = tokens[i] - b; if (t >= 0 && t < rows) atomicOr(&named[t >> 5], 1u << (t & 31)); }
-            __syncthreads();
-            for (int r = 0; r < rows;) {                        // runs of rows without a token
-                int e = r;
-                while (e < rows && !(named[e >> 5] >> (e & 31) & 1)) e = named[e >> 5] == 0 && (e & 31) == 0 ? min(rows, e + 32) : e + 1;
-                if (e > r) zero(dtable, (b + r) * C, (b + e) * C);
-                r = e + 1;
-            }
-        }
+        const long ctas = gridDim.x - sum_ctas, per = (vocab + ctas - 1) / ctas, r0 = (blockIdx.x - sum_ctas) * per;
+        fill_rows<256>([&](int i) { return (long)tok_[i]; }, n, dtable, r0, min(vocab, r0 + per), C, N > 1, named);
         return;
     }
     const int warp = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, i = warp / slices, c = (warp - i * slices) * 32 * N + lane * N;
     if (i >= n) return;
-    const int tok = tokens[i];
+    const int tok = tok_[i];
     if (tok < 0 || tok >= vocab) return;
-    for (int j = 0; j < i; j += 128) {
-        bool same = false;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) { const int q = j + u * 32 + lane; same |= q < i && tokens[q] == tok; }
-        if (__any_sync(~0u, same)) return;
-    }
+    bool same = false;
+    for (int j = lane; j < i; j += 32) same |= tok_[j] == tok;
+    if (__any_sync(~0u, same)) return;
     const bool in = c < C;
     float sum[N] = {};
     for (int j = i; j < n; j += 32) {
-        unsigned hits = __ballot_sync(~0u, j + lane < n && tokens[j + lane] == tok);
+        unsigned hits = __ballot_sync(~0u, j + lane < n && tok_[j + lane] == tok);
         while (hits) {
             Raw<T, N> r[4];
             int m = 0;
@@ -144,108 +155,155 @@ __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ t
 }
 
 // ---- gradient of many tokens
-constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_BITS = 9, MAX_CLUSTER = 8, AHEAD = 8;
+constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CTAS = 148, MAX_BITS = 10;
 
-// entries of the sorted list: token (ids outside the table: vocab, so that they come last) and position
-__global__ void __launch_bounds__(SORT_THREADS) embed_sort_k(const int32_t* __restrict__ tokens, int n, unsigned vocab, uint2* buf0, uint2* buf1, int passes, int bits, int S,
-                                                             float* dtable, long fill) {
-    if (blockIdx.x >= S) {                                      // not the sorting cluster
-        const long ctas = gridDim.x - S, per = ((fill + ctas - 1) / ctas + 3) / 4 * 4, lo = min(fill, (blockIdx.x - S) * per);
-        zero(dtable, lo, min(fill, lo + per));
-        return;
-    }
+// the lanes whose d is this one's, by ballots: __match_any_sync takes longer for 32 different values (a sort 89 us instead of 56)
+__device__ __forceinline__ unsigned equals(unsigned d, int bits) {
+    unsigned m = ~0u;
+    for (int b = 0; b < bits; ++b) { const bool on = d >> b & 1; const unsigned v = __ballot_sync(~0u, on); m &= on ? v : ~v; }
+    return m;
+}
+
+// The list: entries {token, position} by token, then position; tokens outside the table are not in it.  *count: its length.
+__global__ void __launch_bounds__(SORT_THREADS, 1) embed_sort_k(const int32_t* __restrict__ tokens, int n, long vocab, uint2* list, uint2* other, long rows, int passes, int bits,
+                                                               float* dtable, int C, int vec, unsigned* count, unsigned* chains) {
     extern __shared__ unsigned hist[];                          // [warp][bin]
-    __shared__ unsigned total[1 << MAX_BITS], base[1 << MAX_BITS], sums[SORT_WARPS];
-    cg::cluster_group cl = cg::this_cluster();
-    const int rank = blockIdx.x, w = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
-    const int per_warp = ((n + S * SORT_WARPS - 1) / (S * SORT_WARPS) + 31) / 32 * 32;
-    const long b0 = (long)(rank * SORT_WARPS + w) * per_warp;
-    const int begin = (int)min((long)n, b0), end = (int)min((long)n, b0 + per_warp);
-    unsigned* const mine = hist + w * bins;
+    __shared__ unsigned sums[SORT_WARPS], less[SORT_WARPS];
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long first = blockIdx.x * rows, last = min(vocab, first + rows);
+    const unsigned r0 = (unsigned)first, span = (unsigned)(last - first);
+    const bool aligned = (uintptr_t)tokens % 16 == 0;
+    // tokens of the warp, 128 at a time, four consecutive ones a lane, to f(first position, the four)
+    const int per_warp = (int)(((n + SORT_WARPS - 1l) / SORT_WARPS + 127) / 128 * 128);
+    const int begin = (int)min((long)n, (long)w * per_warp), end = (int)min((long)n, (long)(w + 1) * per_warp);
+    auto each = [&](auto f) {
+        constexpr int AHEAD = 4;
+        for (int i0 = begin; i0 < end; i0 += 128 * AHEAD) {
+            uint4 t[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int i = i0 + u * 128 + lane * 4;
+                if (aligned && i + 3 < end) t[u] = *(const uint4*)(tokens + i);
+                else t[u] = make_uint4(i < end ? tokens[i] : ~0u, i + 1 < end ? tokens[i + 1] : ~0u, i + 2 < end ? tokens[i + 2] : ~0u, i + 3 < end ? tokens[i + 3] : ~0u);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) if (i0 + u * 128 < end) f(i0 + u * 128 + lane * 4, t[u]);
+        }
+    };
+    // how many are smaller than the range, how many are the warp's in it
+    unsigned mine = 0, smaller = 0;
+    each([&](int, const uint4& t) {
+        mine += (t.x - r0 < span) + (t.y - r0 < span) + (t.z - r0 < span) + (t.w - r0 < span);
+        smaller += (t.x < r0) + (t.y < r0) + (t.z < r0) + (t.w < r0);
+    });
+    mine = __reduce_add_sync(~0u, mine); smaller = __reduce_add_sync(~0u, smaller);
+    if (lane == 0) { sums[w] = mine; less[w] = smaller; }
+    __syncthreads();
+    unsigned at = 0, m = 0, base = 0;                           // the warp's place, the range's entries, its place in the list
+    for (int q = 0; q < SORT_WARPS; ++q) { if (q < w) at += sums[q]; m += sums[q]; base += less[q]; }
+    if (threadIdx.x == 0) {
+        if (last == vocab) *count = base + m;
+        if (blockIdx.x == 0) *chains = 0;
+    }
+    // the range's entries, in order
+    uint2* src = (passes & 1 ? other : list) + base;
+    uint2* dst = (passes & 1 ? list : other) + base;
+    each([&](int i, const uint4& t) {
+        const bool a = t.x - r0 < span, b = t.y - r0 < span, c = t.z - r0 < span, d = t.w - r0 < span;
+        if (!__any_sync(~0u, a || b || c || d)) return;
+        const unsigned A = __ballot_sync(~0u, a), B = __ballot_sync(~0u, b), Cc = __ballot_sync(~0u, c), D = __ballot_sync(~0u, d), lt = (1u << lane) - 1;
+        unsigned to = at + __popc(A & lt) + __popc(B & lt) + __popc(Cc & lt) + __popc(D & lt);
+        if (a) src[to++] = make_uint2(t.x, i);
+        if (b) src[to++] = make_uint2(t.y, i + 1);
+        if (c) src[to++] = make_uint2(t.z, i + 2);
+        if (d) src[to++] = make_uint2(t.w, i + 3);
+        at += __popc(A) + __popc(B) + __popc(Cc) + __popc(D);
+    });
+    __syncthreads();
+    // sorted by `bits` bits of the row in the range a pass; a warp has a run of the entries and counts of its own
+    const int bins = 1 << bits, run = (int)((m + SORT_THREADS - 1) / SORT_THREADS * 32);
+    const int lo = (int)min((long)m, (long)w * run), hi = (int)min((long)m, (long)(w + 1) * run);
+    unsigned* const own = hist + w * bins;
     for (int p = 0; p < passes; ++p) {
         const int shift = p * bits;
-        const uint2* const src = p & 1 ? buf0 : buf1;
-        uint2* const dst = p & 1 ? buf1 : buf0;
-        // entries begin + 32 k + lane of the warp, k by k, to f(entry, its digit (or `bins` behind the end), lanes of equal digit)
-        auto each = [&](auto f) {
-            for (int i0 = begin; i0 < end; i0 += 32 * AHEAD) {
-                uint2 e[AHEAD];
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const int i = i0 + u * 32 + lane;
-                    if (i >= end) continue;
-                    if (p == 0) { const unsigned t = (unsigned)tokens[i]; e[u] = make_uint2(t < vocab ? t : vocab, (unsigned)i); }
-                    else e[u] = __ldcg(src + i);
-                }
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    if (i0 + u * 32 >= end) break;
-                    const unsigned d = i0 + u * 32 + lane < end ? e[u].x >> shift & (bins - 1) : (unsigned)bins;
-                    f(e[u], d, __match_any_sync(~0u, d));
-                }
-            }
-        };
         for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_THREADS) hist[i] = 0;
         __syncthreads();
-        each([&](const uint2&, unsigned d, unsigned peers) {
-            if (d < bins && lane == __ffs(peers) - 1) mine[d] += __popc(peers);
+        for (int i = lo; i < hi; i += 32) {
+            const bool in = i + lane < hi;
+            const unsigned d = in ? (__ldcg(&src[i + lane].x) - r0) >> shift & (bins - 1) : 0, peers = equals(d, bits) & __ballot_sync(~0u, in);
+            if (in && lane == __ffs(peers) - 1) own[d] += __popc(peers);
             __syncwarp();
-        });
-        __syncthreads();
-        // of every bin: its entries in the warps in front, in the CTA
-        for (int b = threadIdx.x; b < bins; b += SORT_THREADS) {
-            unsigned run = 0;
-#pragma unroll 8
-            for (int q = 0; q < SORT_WARPS; ++q) { const unsigned t = hist[q * bins + b]; hist[q * bins + b] = run; run += t; }
-            total[b] = run;
         }
-        cl.sync();
-        // where the CTA's part of every bin begins: behind all smaller bins and the CTAs in front
-        unsigned all = 0, front = 0;
+        __syncthreads();
+        // where every warp's part of every bin begins
+        unsigned all = 0;
         const int b = threadIdx.x;
         if (b < bins)
-            for (int r = 0; r < S; ++r) { const unsigned t = *cl.map_shared_rank(&total[b], r); all += t; if (r < rank) front += t; }
+#pragma unroll 8
+            for (int q = 0; q < SORT_WARPS; ++q) { const unsigned t = hist[q * bins + b]; hist[q * bins + b] = all; all += t; }
         unsigned scan = all;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) { const unsigned t = __shfl_up_sync(~0u, scan, d); if (lane >= d) scan += t; }
         if (lane == 31) sums[w] = scan;
         __syncthreads();
-        if (b < bins) {
-            unsigned before = scan - all + front;
-            for (int q = 0; q < w; ++q) before += sums[q];
-            base[b] = before;
-        }
+        unsigned before = scan - all;
+        for (int q = 0; q < w; ++q) before += sums[q];
+        if (b < bins)
+#pragma unroll 8
+            for (int q = 0; q < SORT_WARPS; ++q) hist[q * bins + b] += before;
         __syncthreads();
-        each([&](const uint2& e, unsigned d, unsigned peers) {
-            const unsigned at = d < bins ? mine[d] : 0;
+        for (int i = lo; i < hi; i += 32) {
+            const bool in = i + lane < hi;
+            const uint2 e = in ? __ldcg(src + i + lane) : make_uint2(r0, 0);
+            const unsigned d = (e.x - r0) >> shift & (bins - 1), peers = equals(d, bits) & __ballot_sync(~0u, in), to = own[d];
             __syncwarp();
-            if (d < bins) {
-                if (lane == __ffs(peers) - 1) mine[d] = at + __popc(peers);
-                dst[base[d] + at + __popc(peers & ((1u << lane) - 1))] = e;
+            if (in) {
+                if (lane == __ffs(peers) - 1) own[d] = to + __popc(peers);
+                dst[to + __popc(peers & ((1u << lane) - 1))] = e;
             }
             __syncwarp();
-        });
-        cl.sync();                                              // the list is whole, and nobody reads `total` any more
+        }
+        __syncthreads();
+        uint2* const t = src; src = dst; dst = t;
     }
+    if (dtable) fill_rows<SORT_THREADS>([&](int i) { return (long)__ldcg(&src[i].x); }, (int)m, dtable, first, last, C, vec, hist);
 }
 
 // How the sorted list is cut: tiles of `tile` entries, each summed by teams of `tx` threads (of which `slices` cover the channels).
-struct Plan { int vec, tx, slices, tile; long tiles; };
+struct Plan { int tx, slices, tile, tiles; };
+// What the sums leave for the joins.
+struct Left {
+    float* part;            // [tile][C]: sums of the tokens that began in an earlier tile
+    int* head;              // [tile]: that token, or -1
+    unsigned* count;        // entries of the list
+    unsigned* chains;       // how many tokens go on behind the tile in which they began,
+    int* chain;             // and these tiles, in any order
+};
 
 constexpr int BATCH = 8;                        // rows on their way at once
 template <typename T, int N>
-__global__ void __launch_bounds__(256) embed_sums_k(const uint2* __restrict__ list, int n, const T* __restrict__ dy, long dys, unsigned vocab, int C, float scale, int accum,
-                                                    float* __restrict__ dtable, float* __restrict__ part, Plan p) {
-    const long tile = (long)blockIdx.x * (256 / p.tx) + threadIdx.x / p.tx;
+__global__ void __launch_bounds__(256, 3) embed_sums_k(const uint2* __restrict__ list, const T* __restrict__ dy, long dys, int C, float scale, int accum,
+                                                    float* __restrict__ dtable, Left left, Plan p) {
+    const int tile = blockIdx.x * (256 / p.tx) + threadIdx.x / p.tx;
     const int c = (blockIdx.y * p.tx + threadIdx.x % p.tx) * N;
+    const int n = (int)*left.count, t0 = tile * p.tile, t1 = min(n, t0 + p.tile);
     if (tile >= p.tiles || c >= C) return;
-    const int t0 = (int)(tile * p.tile), t1 = min(n, t0 + p.tile);
+    if (t0 >= n) {                                              // (tokens outside the table have shortened the list)
+        if (c == 0) left.head[tile] = -1;
+        return;
+    }
     unsigned now = list[t0].x;
     bool begun = t0 > 0 && list[t0 - 1].x == now;               // in an earlier tile
+    if (c == 0) {
+        left.head[tile] = begun ? (int)now : -1;
+        if (t1 < n) {                                           // the last token of the tile goes on, and began here
+            const unsigned last = list[t1 - 1].x;
+            if (list[t1].x == last && !(begun && last == now)) left.chain[atomicAdd(left.chains, 1u)] = tile;
+        }
+    }
     float sum[N] = {};
     auto leave = [&]() {
-        if (now >= vocab) return;
-        float* const d = begun ? part + tile * C + c : dtable + (long)now * C + c;
+        float* const d = begun ? left.part + (long)tile * C + c : dtable + (long)now * C + c;
 #pragma unroll
         for (int k = 0; k < N; ++k) sum[k] = begun ? sum[k] : accum ? fmaf(sum[k], scale, d[k]) : sum[k] * scale;
         if constexpr (N >= 4) {                                 // (rows of such tables start on 16 bytes)
@@ -260,9 +318,10 @@ __global__ void __launch_bounds__(256) embed_sums_k(const uint2* __restrict__ li
         Raw<T, N> r[BATCH];
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
-            const uint2 e = i + u < t1 ? list[i + u] : make_uint2(vocab, 0);
+            if (i + u >= t1) continue;
+            const uint2 e = list[i + u];
             key[u] = e.x;
-            if (e.x < vocab) r[u] = *(const Raw<T, N>*)(dy + (long)e.y * dys + c);
+            r[u] = *(const Raw<T, N>*)(dy + (long)e.y * dys + c);
         }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
@@ -273,51 +332,60 @@ __global__ void __launch_bounds__(256) embed_sums_k(const uint2* __restrict__ li
 #pragma unroll
                 for (int k = 0; k < N; ++k) sum[k] = 0.f;
             }
-            if (now < vocab) {
-                float x[N];
-                unpack<T, N>(r[u], x);
+            float x[N];
+            unpack<T, N>(r[u], x);
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] += x[k];
-            }
+            for (int k = 0; k < N; ++k) sum[k] += x[k];
         }
     }
     leave();
 }
 
-// Here a thread has 4 channels (N = 4, rows on 16 bytes) or one; tx of them make a team.
-constexpr int JOIN_BATCH = 16;
+// A CTA per such token and JOIN_TX threads' channels, of 4 (N = 4, rows on 16 bytes) or one: its groups of threads add equal runs of the tiles that follow, then the groups are
+// added in order.
+constexpr int JOIN_TX = 64, JOIN_GROUPS = 256 / JOIN_TX, JOIN_BATCH = 8;
 template <int N>
-__global__ void __launch_bounds__(256) embed_joins_k(const uint2* __restrict__ list, int n, unsigned vocab, int C, float scale, float* __restrict__ dtable,
-                                                     const float* __restrict__ part, long tiles, int tile_, int tx) {
-    const long tile = (long)blockIdx.x * (256 / tx) + threadIdx.x / tx;
-    const int c = (blockIdx.y * tx + threadIdx.x % tx) * N;
-    if (tile + 1 >= tiles || c >= C) return;
-    const long t0 = tile * tile_, t1 = t0 + tile_;
-    const unsigned now = list[t1 - 1].x;
-    if (now >= vocab || list[t1].x != now) return;              // nothing goes on behind this tile
-    if (t0 > 0 && list[t0].x == now && list[t0 - 1].x == now) return;        // it began before this tile
-    float sum[N] = {};
-    for (long j = tile + 1; j < tiles; j += JOIN_BATCH) {
-        bool more[JOIN_BATCH];
-        Raw<float, N> v[JOIN_BATCH];
-#pragma unroll
-        for (int u = 0; u < JOIN_BATCH; ++u) {
-            more[u] = j + u < tiles && list[(j + u) * tile_].x == now;
-            if (more[u]) v[u] = *(const Raw<float, N>*)(part + (j + u) * C + c);
+__global__ void __launch_bounds__(256) embed_joins_k(int C, float scale, float* __restrict__ dtable, Left left, Plan p) {
+    __shared__ float sums[JOIN_GROUPS][JOIN_TX * N];
+    const int c = (blockIdx.y * JOIN_TX + threadIdx.x % JOIN_TX) * N, group = threadIdx.x / JOIN_TX, all = (int)*left.chains;
+    for (int e = blockIdx.x; e < all; e += gridDim.x) {
+        const int first = left.chain[e] + 1, now = left.head[first];
+        int length = 0;                                         // tiles that it goes on through
+        for (int j = first;; j += 256) {
+            const int more = __syncthreads_count(j + (int)threadIdx.x < p.tiles && left.head[j + threadIdx.x] == now);
+            length += more;
+            if (more < 256) break;
         }
+        const int run = (length + JOIN_GROUPS - 1) / JOIN_GROUPS, lo = first + group * run, hi = min(first + length, lo + run);
+        float sum[N] = {};
+        if (c < C)
+            for (int j = lo; j < hi; j += JOIN_BATCH) {
+                Raw<float, N> v[JOIN_BATCH];
 #pragma unroll
-        for (int u = 0; u < JOIN_BATCH; ++u)
-            if (more[u]) {
-                float x[N];
-                unpack<float, N>(v[u], x);
+                for (int u = 0; u < JOIN_BATCH; ++u) if (j + u < hi) v[u] = *(const Raw<float, N>*)(left.part + (long)(j + u) * C + c);
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] += x[k];
+                for (int u = 0; u < JOIN_BATCH; ++u)
+                    if (j + u < hi) {
+                        float x[N];
+                        unpack<float, N>(v[u], x);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) sum[k] += x[k];
+                    }
             }
-        if (!more[JOIN_BATCH - 1]) break;
-    }
-    float* const d = dtable + (long)now * C + c;
 #pragma unroll
-    for (int k = 0; k < N; ++k) d[k] = fmaf(sum[k], scale, d[k]);
+        for (int k = 0; k < N; ++k) sums[group][threadIdx.x % JOIN_TX * N + k] = sum[k];
+        __syncthreads();
+        if (group == 0 && c < C) {
+            float* const d = dtable + (long)now * C + c;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                float t = sum[k];
+#pragma unroll
+                for (int q = 1; q < JOIN_GROUPS; ++q) t += sums[q][threadIdx.x * N + k];
+                d[k] = fmaf(t, scale, d[k]);
+            }
+        }
+    }
 }
 
 // elements that may be moved at once
@@ -327,7 +395,7 @@ template <typename T> int vector(const void* a, long stride_a, long C) {
 }
 
 int log2_up(long v) { int b = 0; while (1l << b < v) ++b; return b; }
-// vec: as the rows' alignment allows (it moves the teams' borders, not a sum's order: that is given by the tiles, which come from the sizes)
+// vec: elements of a thread, as the rows' alignment allows (it moves the teams' borders, not a sum's order: that is given by the tiles, which come from the sizes)
 Plan plan(int dt, long n, long C, int vec) {
     Plan p;
     const int most = dt ? 8 : 4;
@@ -336,12 +404,23 @@ Plan plan(int dt, long n, long C, int vec) {
     int t = 16;
     while (t < 128 && (n / (2 * t)) * threads >= 148l * 512) t *= 2;
     p.tile = t;
-    p.tiles = (n + t - 1) / t;
-    p.vec = vec;
+    p.tiles = (int)((n + t - 1) / t);
     p.tx = 1 << std::min(8, log2_up((C + vec - 1) / vec));
     p.slices = (int)(((C + vec - 1) / vec + p.tx - 1) / p.tx);
     return p;
 }
+// The workspace: two lists of the sort, and what the sums leave.
+struct Space {
+    size_t list, part, head, chain, bytes;
+    Space(long n, long tiles, long C) {
+        auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+        list = up((size_t)n * sizeof(uint2));
+        part = 2 * list;
+        head = part + up((size_t)tiles * C * sizeof(float));
+        chain = head + up((size_t)tiles * sizeof(int));
+        bytes = chain + up((size_t)(tiles + 2) * sizeof(int));
+    }
+};
 
 template <typename T>
 cudaError_t forward_t(const int32_t* tokens, long n, const void* table, long vocab, long C, float scale, void* y, long ys, cudaStream_t s) {
@@ -360,27 +439,24 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
         return klaunch(embed_few_k<T, N>, (unsigned)(sum_ctas + fill_ctas), 256, 0, s, tokens, (int)n, dy, dys, vocab, (int)C, slices, scale, (int)accum, dtable, sum_ctas);
     }
     const Plan p = plan(dt, n, C, N);
-    const size_t list_bytes = ((size_t)n * sizeof(uint2) + 255) / 256 * 256;
-    uint2 *const buf0 = (uint2*)ws, *const buf1 = (uint2*)(ws + list_bytes);
-    float* const part = (float*)(ws + 2 * list_bytes);
-    const int key_bits = log2_up(vocab + 1), passes = (key_bits + MAX_BITS - 1) / MAX_BITS, bits = (key_bits + passes - 1) / passes;
-    int S = 1;
-    while (S < MAX_CLUSTER && n > 2048l * S) S *= 2;
-    const long fill = accum ? 0 : vocab * C;
-    const int fill_ctas = (int)(std::min<long>((fill + 65535) / 65536, 2 * 148) + S - 1) / S * S;
-    const size_t smem = (size_t)SORT_WARPS * (1 << bits) * sizeof(unsigned);
+    const Space sp(n, p.tiles, C);
+    uint2 *const list = (uint2*)ws, *const other = (uint2*)(ws + sp.list);
+    unsigned* const counts = (unsigned*)(ws + sp.chain);
+    const Left left{(float*)(ws + sp.part), (int*)(ws + sp.head), counts, counts + 1, (int*)counts + 2};
+    const long rows = (vocab + SORT_CTAS - 1) / SORT_CTAS;
+    const int key_bits = std::max(1, log2_up(rows)), passes = (key_bits + MAX_BITS - 1) / MAX_BITS, bits = (key_bits + passes - 1) / passes;
     static OncePerDevice once;
-    cudaError_t e = allow_smem(once, (const void*)embed_sort_k, SORT_WARPS * (1 << MAX_BITS) * sizeof(unsigned));
+    cudaError_t e = allow_smem(once, (const void*)embed_sort_k, SORT_WARPS * (1 << MAX_BITS) * (int)sizeof(unsigned));
     if (e != cudaSuccess) return e;
-    e = klaunch_cluster(embed_sort_k, (unsigned)(S + fill_ctas), SORT_THREADS, smem, s, S, tokens, (int)n, (unsigned)vocab, buf0, buf1, passes, bits, S, dtable, fill);
+    e = klaunch(embed_sort_k, (unsigned)((vocab + rows - 1) / rows), SORT_THREADS, (size_t)std::max(SORT_WARPS << bits, FILL_ROWS / 32) * sizeof(unsigned), s, tokens, (int)n, vocab,
+                list, other, rows, passes, bits, accum ? nullptr : dtable, (int)C, (int)(N > 1), left.count, left.chains);
     if (e != cudaSuccess) return e;
-    const uint2* const list = passes & 1 ? buf0 : buf1;
     const dim3 grid((unsigned)((p.tiles + 256 / p.tx - 1) / (256 / p.tx)), (unsigned)p.slices);
-    e = klaunch(embed_sums_k<T, N>, grid, 256, 0, s, list, (int)n, dy, dys, (unsigned)vocab, (int)C, scale, (int)accum, dtable, part, p);
+    e = klaunch(embed_sums_k<T, N>, grid, 256, 0, s, (const uint2*)list, dy, dys, (int)C, scale, (int)accum, dtable, left, p);
     if (e != cudaSuccess || p.tiles == 1) return e;
-    const int jv = N > 1 ? 4 : 1, tx = 1 << std::min(8, log2_up((C + jv - 1) / jv));
-    const dim3 jgrid((unsigned)((p.tiles + 256 / tx - 1) / (256 / tx)), (unsigned)((C + (long)jv * tx - 1) / ((long)jv * tx)));
-    return klaunch(embed_joins_k<(N > 1 ? 4 : 1)>, jgrid, 256, 0, s, list, (int)n, (unsigned)vocab, (int)C, scale, dtable, (const float*)part, p.tiles, p.tile, tx);
+    constexpr int J = N > 1 ? 4 : 1;
+    const dim3 joins((unsigned)std::min(p.tiles, 4 * 148), (unsigned)((C + J * JOIN_TX - 1) / (J * JOIN_TX)));
+    return klaunch(embed_joins_k<J>, joins, 256, 0, s, (int)C, scale, dtable, left, p);
 }
 
 }  // namespace
@@ -393,8 +469,7 @@ cudaError_t embed_forward(int dt, const int32_t* tokens, long n, const void* tab
 
 size_t embed_workspace_bytes(long n, long, long C) {
     if (n <= FEW) return 0;
-    const long tiles = std::max(plan(0, n, C, 1).tiles, plan(1, n, C, 1).tiles);
-    return 2 * (((size_t)n * sizeof(uint2) + 255) / 256 * 256) + (size_t)tiles * C * sizeof(float);
+    return Space(n, std::max(plan(0, n, C, 1).tiles, plan(1, n, C, 1).tiles), C).bytes;
 }
 
 cudaError_t embed_backward(int dt, const int32_t* tokens, long n, const void* dy, long dy_stride, long vocab, long C, float scale, bool accum, float* dtable, void* ws,

@@ -52,7 +52,8 @@ def _tokens(g, n, vocab, kind):
 
 # ---- embedding
 
-EMBED = [(1, 1, 1), (1, 10, 8), (5, 3, 7), (33, 1000, 100), (64, 2, 64), (257, 70001, 24), (1000, 50, 129), (2100, 300, 40), (700, 128, 1024), (300, 37, 2050)]
+EMBED = [(1, 1, 1), (1, 10, 8), (5, 3, 7), (33, 1000, 100), (64, 2, 64), (257, 70001, 24), (512, 9000, 36), (513, 1, 5), (1000, 50, 129), (2100, 300, 40), (700, 128, 1024),
+         (300, 37, 2050), (1025, 148, 12), (1537, 149, 3)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)
@@ -107,7 +108,7 @@ def test_embedding_gradient(ops, n, vocab, c, kind, dtype):
 
 
 @pytest.mark.parametrize("kind", ["uniform", "padded", "one", "skewed"])
-@pytest.mark.parametrize("n,vocab,c", [(9000, 1000, 64), (40000, 33000, 16), (70000, 300000, 8), (150001, 17, 40)])
+@pytest.mark.parametrize("n,vocab,c", [(9000, 1000, 64), (40000, 33000, 16), (70000, 300000, 8), (150001, 17, 40), (3000, 4000003, 2)])
 def test_embedding_gradient_of_many_tokens(ops, n, vocab, c, kind):
     g = _gen("many", n, vocab, c, kind)
     tok = _tokens(g, n, vocab, kind)
