@@ -6,7 +6,8 @@
 // Few tokens: a warp per token looks through all of them.  Otherwise the positions are sorted by token (stable) and the sorted list is cut into tiles:
 //   sort    every CTA owns a range of the table's rows: it picks the tokens of its range out of all (and counts the smaller ones, so it knows its place in the
 //           list without asking anyone), sorts them, and fills the rows that none names with zeros.  Reading all tokens in every CTA costs 1 us per 8000;
-//           a cluster that sorted for all took 56 us for 131072 tokens beside SMs that waited
+//           a cluster that sorted for all took 56 us for 131072 tokens, this 28.  (All rows filled from the start, beside the sort: 112 instead of 104 us for
+//           131072 rows of 1024, of which 46000 occur; HBM takes writes alone at 4.8 to 5.5 TB/s, so those that are written anyway are better left out.)
 //   sums    a team of threads per tile adds the rows up, and writes a token's sum when the next one begins; a sum that began in an earlier tile is left as
 //           a partial row
 //   joins   the team of the tile in which a token began adds the partial rows of the following tiles to its row
@@ -277,7 +278,7 @@ struct Left {
     int* head;              // [tile]: that token, or -1
     unsigned* count;        // entries of the list
     unsigned* chains;       // how many tokens go on behind the tile in which they began,
-    int* chain;             // and these tiles, in any order
+    int2* chain;            // and these tiles and tokens, in any order
 };
 
 constexpr int BATCH = 8;                        // rows on their way at once
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(256, 3) embed_sums_k(const uint2* __restrict__
         left.head[tile] = begun ? (int)now : -1;
         if (t1 < n) {                                           // the last token of the tile goes on, and began here
             const unsigned last = list[t1 - 1].x;
-            if (list[t1].x == last && !(begun && last == now)) left.chain[atomicAdd(left.chains, 1u)] = tile;
+            if (list[t1].x == last && !(begun && last == now)) left.chain[atomicAdd(left.chains, 1u)] = make_int2(tile, (int)last);
         }
     }
     float sum[N] = {};
@@ -347,9 +348,21 @@ constexpr int JOIN_TX = 64, JOIN_GROUPS = 256 / JOIN_TX, JOIN_BATCH = 8;
 template <int N>
 __global__ void __launch_bounds__(256) embed_joins_k(int C, float scale, float* __restrict__ dtable, Left left, Plan p) {
     __shared__ float sums[JOIN_GROUPS][JOIN_TX * N];
-    const int c = (blockIdx.y * JOIN_TX + threadIdx.x % JOIN_TX) * N, group = threadIdx.x / JOIN_TX, all = (int)*left.chains;
+    const int c = (blockIdx.y * JOIN_TX + threadIdx.x % JOIN_TX) * N, group = threadIdx.x / JOIN_TX;
+    const unsigned* const chains = left.chains;
+    int2 next = left.chain[blockIdx.x];                         // (whether it is one of them or not: the loads wait for nothing)
+    const int all = (int)*chains;
     for (int e = blockIdx.x; e < all; e += gridDim.x) {
-        const int first = left.chain[e] + 1, now = left.head[first];
+        const int first = next.x + 1, now = next.y;
+        if (e + (int)gridDim.x < all) next = left.chain[e + gridDim.x];
+        float* const d = dtable + (long)now * C + c;
+        Raw<float, N> old{};
+        if (group == 0 && c < C) {
+            float x[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = d[k];
+            old = pack<float, N>(x);
+        }
         int length = 0;                                         // tiles that it goes on through
         for (int j = first;; j += 256) {
             const int more = __syncthreads_count(j + (int)threadIdx.x < p.tiles && left.head[j + threadIdx.x] == now);
@@ -376,13 +389,14 @@ __global__ void __launch_bounds__(256) embed_joins_k(int C, float scale, float* 
         for (int k = 0; k < N; ++k) sums[group][threadIdx.x % JOIN_TX * N + k] = sum[k];
         __syncthreads();
         if (group == 0 && c < C) {
-            float* const d = dtable + (long)now * C + c;
+            float x[N];
+            unpack<float, N>(old, x);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 float t = sum[k];
 #pragma unroll
                 for (int q = 1; q < JOIN_GROUPS; ++q) t += sums[q][threadIdx.x * N + k];
-                d[k] = fmaf(t, scale, d[k]);
+                d[k] = fmaf(t, scale, x[k]);
             }
         }
     }
@@ -418,7 +432,7 @@ struct Space {
         part = 2 * list;
         head = part + up((size_t)tiles * C * sizeof(float));
         chain = head + up((size_t)tiles * sizeof(int));
-        bytes = chain + up((size_t)(tiles + 2) * sizeof(int));
+        bytes = chain + up((size_t)(tiles + 1) * sizeof(int2));
     }
 };
 
@@ -442,7 +456,7 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
     const Space sp(n, p.tiles, C);
     uint2 *const list = (uint2*)ws, *const other = (uint2*)(ws + sp.list);
     unsigned* const counts = (unsigned*)(ws + sp.chain);
-    const Left left{(float*)(ws + sp.part), (int*)(ws + sp.head), counts, counts + 1, (int*)counts + 2};
+    const Left left{(float*)(ws + sp.part), (int*)(ws + sp.head), counts, counts + 1, (int2*)(counts + 2)};
     const long rows = (vocab + SORT_CTAS - 1) / SORT_CTAS;
     const int key_bits = std::max(1, log2_up(rows)), passes = (key_bits + MAX_BITS - 1) / MAX_BITS, bits = (key_bits + passes - 1) / passes;
     static OncePerDevice once;
@@ -455,7 +469,7 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
     e = klaunch(embed_sums_k<T, N>, grid, 256, 0, s, (const uint2*)list, dy, dys, (int)C, scale, (int)accum, dtable, left, p);
     if (e != cudaSuccess || p.tiles == 1) return e;
     constexpr int J = N > 1 ? 4 : 1;
-    const dim3 joins((unsigned)std::min(p.tiles, 4 * 148), (unsigned)((C + J * JOIN_TX - 1) / (J * JOIN_TX)));
+    const dim3 joins((unsigned)std::min(p.tiles, 8 * 148), (unsigned)((C + J * JOIN_TX - 1) / (J * JOIN_TX)));
     return klaunch(embed_joins_k<J>, joins, 256, 0, s, (int)C, scale, dtable, left, p);
 }
 
