@@ -26,7 +26,7 @@
  *   - Activations are NHWC, worker-major: rows s*B .. (s+1)*B-1 belong to worker s.
  *   - Canonical parameter order: layers in list order; per layer W then b (linear W[out][in];
  *     conv W[c_out][kh][kw][c_in]); batch-norm gamma then beta; a projecting FDG_RES_ADD
- *     carries Wp[c_out][c_in], gamma_p, beta_p.
+ *     carries Wp[c_out][c_in], gamma_p, beta_p; an embedding its table W[c_in][c_out].
  *   - The library needs an sm_100 device; there is no CPU path.
  *   - Threads: calls on one context must not overlap in time; different contexts are independent.  Everything a
  *     call enqueues runs asynchronously on the context's streams.
@@ -70,10 +70,17 @@ typedef enum {
     FDG_GLOBAL_AVGPOOL = 5,
     FDG_BATCHNORM = 6,         /* per-worker batch statistics                                   */
     FDG_RES_BEGIN = 7,         /* remember the current tensor as the shortcut                   */
-    FDG_RES_ADD = 8            /* add the shortcut (flags & 1: through conv1x1(stride) + BN)    */
+    FDG_RES_ADD = 8,           /* add the shortcut (flags & 1: through conv1x1(stride) + BN)    */
+    FDG_EMBEDDING = 9,         /* the network's first layer: rows of a table [c_in][c_out] for token ids.  in_c is 1; the
+                                  inputs of a step are then int32 ids [M][in_h][in_w] whatever the dtype.  An id outside
+                                  0..c_in-1 (padding) gives zeros.  flags & 1: times sqrt(c_out)            */
+    FDG_RECURRENCE = 10        /* gated linear recurrence along a sample's positions (rows of the image one after the
+                                  other) from a zero state, c_in = 2 c_out: channels 0..c_out-1 are the gates, the others
+                                  the values (see fdg_recurrence_forward)                                   */
 } fdg_layer_kind;
 
-/* flags: bit 0 = has bias (LINEAR / CONV*), or "projection shortcut" (RES_ADD). */
+/* flags: bit 0 = has bias (LINEAR / CONV*), "projection shortcut" (RES_ADD), or "scaled" (EMBEDDING).
+ * A module with an EMBEDDING or a RECURRENCE layer runs over all workers at once (worker_groups is ignored there). */
 typedef struct { int32_t kind, c_in, c_out, stride, flags; } fdg_layer;
 
 /* Device-memory allocator of the caller (e.g. PyTorch's caching allocator).  alloc returns a
@@ -158,7 +165,7 @@ FDG_API fdg_status fdg_param_count(const fdg_ctx* ctx, size_t* count);
  * g(k) = {p_k .. q_k} of Sec. 3.2.
  *   layer  : index into the layer list given to fdg_create
  *   module : k - 1 of the module that owns the layer
- *   role   : FDG_PARAM_W (linear [out][in]; conv [c_out][kh][kw][c_in]), _BIAS, _GAMMA, _BETA, and for a projecting
+ *   role   : FDG_PARAM_W (linear [out][in]; conv [c_out][kh][kw][c_in]; embedding [c_in][c_out]), _BIAS, _GAMMA, _BETA, and for a projecting
  *            FDG_RES_ADD  _PROJ_W [c_out][1][1][c_in], _PROJ_GAMMA, _PROJ_BETA
  *   ndim, shape[4] : extents, outermost first (unused trailing extents are 1)
  *   offset, count  : first element and number of elements in the canonical vector
@@ -192,6 +199,15 @@ FDG_API fdg_status fdg_set_params_worker(fdg_ctx* ctx, int32_t worker, const flo
  *                in flight when the call returns.  If NULL the call only enqueues work. */
 FDG_API fdg_status fdg_step(fdg_ctx* ctx, const void* dev_inputs, const int32_t* dev_labels,
                     float* host_loss_or_null);
+
+/* Train against a teacher as well: from now on the loss of a sample is that of fdg_distill_loss, with `top` of the teacher's logits per sample, and a sample
+ * whose label is outside 0..num_classes-1 does not count (its loss and gradient are zero; the means over M count it).  Call it before the first step
+ * (FDG_ERR_STATE later, or a second time); num_classes <= 262144, 1 <= top <= 1024, temperature and weight as there.  The steps are then
+ * fdg_step_distill's: fdg_step and fdg_step_host return FDG_ERR_STATE. */
+FDG_API fdg_status fdg_set_distill(fdg_ctx* ctx, int32_t top, float temperature, float weight);
+/* fdg_step with the teacher's entries of the same batch: ids int32 [M][top] (outside 0..num_classes-1: no entry), teacher fp32 [M][top].  The buffers are device
+ * or pinned host memory, complete before the call; all four are copied, as fdg_step_host does (fdg_wait_ingest tells when). */
+FDG_API fdg_status fdg_step_distill(fdg_ctx* ctx, const void* inputs, const int32_t* labels, const int32_t* ids, const float* teacher, float* host_loss_or_null);
 
 /* Same as fdg_step with HOST input buffers (pinned memory makes the copies asynchronous); the
  * host-to-device copies go straight into the FIFO slot.  With fdg_options.streams (or serial = 1) they are

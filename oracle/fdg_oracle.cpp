@@ -45,7 +45,7 @@
 
 namespace {
 
-enum Kind { LINEAR = 0, CONV3X3, CONV1X1, RELU, MAXPOOL2, GLOBAL_AVGPOOL, BATCHNORM, RES_BEGIN, RES_ADD };
+enum Kind { LINEAR = 0, CONV3X3, CONV1X1, RELU, MAXPOOL2, GLOBAL_AVGPOOL, BATCHNORM, RES_BEGIN, RES_ADD, EMBEDDING, RECURRENCE };
 struct Layer { int32_t kind, c_in, c_out, stride, flags; };
 constexpr double BN_EPS = 1e-5;
 
@@ -116,6 +116,7 @@ size_t layer_param_count(const Layer& L) {
         case CONV3X3: return (size_t)9 * L.c_in * L.c_out + ((L.flags & 1) ? L.c_out : 0);
         case CONV1X1: return (size_t)L.c_in * L.c_out + ((L.flags & 1) ? L.c_out : 0);
         case BATCHNORM: return (size_t)2 * L.c_in;
+        case EMBEDDING: return (size_t)L.c_in * L.c_out;
         case RES_ADD: return (L.flags & 1) ? (size_t)L.c_in * L.c_out + 2 * (size_t)L.c_out : 0;
         default: return 0;
     }
@@ -281,6 +282,95 @@ Tensor bn_bwd(const Tensor& x, const Tensor& gy, const double* gamma, const BnSa
     return g;
 }
 
+// Embedding: rows of the table W[vocab][c] for ids (held as numbers), zeros for ids outside it; flags & 1: times sqrt(c), as fp32 has it.
+double embed_scale(const Layer& Y) { return (Y.flags & 1) ? (double)std::sqrt((float)Y.c_out) : 1.0; }
+Tensor embed_fwd(const Tensor& x, const Layer& Y, const double* W) {
+    Tensor y(x.n, x.h, x.w, Y.c_out);
+    for (size_t p = 0; p < x.v.size(); ++p) {
+        const double id = x.v[p];
+        if (id < 0 || id >= Y.c_in) continue;
+        for (int c = 0; c < Y.c_out; ++c) y.v[p * Y.c_out + c] = embed_scale(Y) * W[(size_t)id * Y.c_out + c];
+    }
+    return y;
+}
+void embed_bwd(const Tensor& x, const Layer& Y, const Tensor& gy, double* gW) {
+    for (size_t p = 0; p < x.v.size(); ++p) {
+        const double id = x.v[p];
+        if (id < 0 || id >= Y.c_in) continue;
+        for (int c = 0; c < Y.c_out; ++c) gW[(size_t)id * Y.c_out + c] += embed_scale(Y) * gy.v[p * Y.c_out + c];
+    }
+}
+
+// Gated linear recurrence along a sample's positions: a = sigmoid(z), h_t = a h_{t-1} + (1 - a) v_t from h_0 = 0; x holds z, then v.
+Tensor recur_fwd(const Tensor& x) {
+    const int C = x.c / 2, T = x.h * x.w;
+    Tensor y(x.n, x.h, x.w, C);
+    for (int i = 0; i < x.n; ++i) for (int c = 0; c < C; ++c) {
+        double h = 0.0;
+        for (int t = 0; t < T; ++t) {
+            const double* p = x.v.data() + ((size_t)i * T + t) * x.c;
+            const double a = 1.0 / (1.0 + std::exp(-p[c]));
+            h = a * h + (1.0 - a) * p[C + c];
+            y.v[((size_t)i * T + t) * C + c] = h;
+        }
+    }
+    return y;
+}
+// The states are computed again (y as it was stored may be rounded).
+Tensor recur_bwd(const Tensor& x, const Tensor& gy) {
+    const int C = x.c / 2, T = x.h * x.w;
+    const Tensor h = recur_fwd(x);
+    Tensor g(x.n, x.h, x.w, x.c);
+    for (int i = 0; i < x.n; ++i) for (int c = 0; c < C; ++c) {
+        double later = 0.0;                        // a_{t+1} times the gradient of h_{t+1}
+        for (int t = T - 1; t >= 0; --t) {
+            const size_t at = (size_t)i * T + t;
+            const double* p = x.v.data() + at * x.c;
+            const double a = 1.0 / (1.0 + std::exp(-p[c])), d = gy.v[at * C + c] + later, before = t ? h.v[(at - 1) * C + c] : 0.0;
+            g.v[at * x.c + c] = a * (1.0 - a) * d * (before - p[C + c]);
+            g.v[at * x.c + C + c] = (1.0 - a) * d;
+            later = a * d;
+        }
+    }
+    return g;
+}
+
+// Distillation per sample: w tau^2 KL(teacher | student) over the teacher's entries at temperature tau plus (1 - w) cross-entropy; a label outside the classes
+// takes the sample out.
+struct Distill { int top = 0; double tau = 1.0, weight = 1.0; };
+double distill_loss(const Tensor& logits, const int32_t* labels, const int32_t* ids, const double* teacher, const Distill& D, double scale, Tensor* g) {
+    const int C = logits.c;
+    double total = 0.0;
+    *g = Tensor(logits.n, 1, 1, C);
+    for (int i = 0; i < logits.n; ++i) {
+        const double* z = logits.v.data() + (size_t)i * C;
+        double* gi = g->v.data() + (size_t)i * C;
+        if (labels[i] < 0 || labels[i] >= C) continue;
+        auto lse = [&](double tau) {
+            double m = z[0]; for (int c = 1; c < C; ++c) m = std::max(m, z[c]);
+            double se = 0.0; for (int c = 0; c < C; ++c) se += std::exp((z[c] - m) / tau);
+            return m / tau + std::log(se);
+        };
+        const double lt = lse(D.tau), l1 = lse(1.0);
+        double tm = -INFINITY, ts = 0.0;
+        for (int j = 0; j < D.top; ++j) { const int id = ids[i * D.top + j]; if (id >= 0 && id < C) tm = std::max(tm, teacher[i * D.top + j]); }
+        if (tm > -INFINITY) {
+            for (int j = 0; j < D.top; ++j) { const int id = ids[i * D.top + j]; if (id >= 0 && id < C) ts += std::exp((teacher[i * D.top + j] - tm) / D.tau); }
+            for (int c = 0; c < C; ++c) gi[c] += scale * D.weight * D.tau * std::exp(z[c] / D.tau - lt);
+            for (int j = 0; j < D.top; ++j) {
+                const int id = ids[i * D.top + j];
+                if (id < 0 || id >= C) continue;
+                const double lp = (teacher[i * D.top + j] - tm) / D.tau - std::log(ts), p = std::exp(lp);
+                if (p > 0.0) total += D.weight * D.tau * D.tau * p * (lp - (z[id] / D.tau - lt));
+                gi[id] -= scale * D.weight * D.tau * p;
+            }
+        }
+        total += (1.0 - D.weight) * (l1 - z[labels[i]]);
+        for (int c = 0; c < C; ++c) gi[c] += scale * (1.0 - D.weight) * (std::exp(z[c] - l1) - (c == labels[i] ? 1.0 : 0.0));
+    }
+    return total;
+}
+
 // Softmax cross-entropy per sample; returns the summed loss, writes scale * (softmax - onehot).
 double softmax_ce(const Tensor& logits, const int32_t* labels, double scale, Tensor* g) {
     int C = logits.c; double total = 0.0;
@@ -328,6 +418,8 @@ Tensor group_forward(const std::vector<Layer>& L, int p, int q, const double* pr
             case GLOBAL_AVGPOOL: sv->in[j] = x; x = gap_fwd(x); store(x, sq); break;
             case BATCHNORM: sv->in[j] = x; x = bn_fwd(x, w, w + Y.c_in, &sv->bn[j]);
                 store(x, sq && !(l + 1 < q && L[l + 1].kind == RES_ADD)); break;
+            case EMBEDDING: sv->in[j] = x; x = embed_fwd(x, Y, w); store(x, sq); break;
+            case RECURRENCE: sv->in[j] = x; x = recur_fwd(x); store(x, sq); break;
             case RES_BEGIN: shortcut.push_back(x); break;
             case RES_ADD: {
                 Tensor s = shortcut.back(); shortcut.pop_back();
@@ -374,6 +466,8 @@ Tensor group_backward(const std::vector<Layer>& L, int p, int q, const double* p
                 }
                 break; }
             case RELU: g = relu_bwd(sv.in[j], g); break;
+            case EMBEDDING: embed_bwd(sv.in[j], Y, g, gw); break;
+            case RECURRENCE: g = recur_bwd(sv.in[j], g); store(g, sq && !(l > p && L[l - 1].kind == RES_BEGIN)); break;
             case MAXPOOL2: g = maxpool_bwd(sv.in[j], g); break;
             case GLOBAL_AVGPOOL: g = gap_bwd(sv.in[j], g); store(g, sq); break;
             case BATCHNORM: g = bn_bwd(sv.in[j], g, w, sv.bn[j], gw, gw + Y.c_in); store(g, sq); break;
@@ -402,7 +496,7 @@ Tensor group_backward(const std::vector<Layer>& L, int p, int q, const double* p
 
 // ---------------------------------------------------------------- the S x K agents
 
-struct Message { long batch = -1; Tensor t; std::vector<int32_t> labels; };
+struct Message { long batch = -1; Tensor t; std::vector<int32_t> labels, ids; std::vector<double> teacher; };
 struct StashEntry { long version; std::vector<double> w; Saved sv; std::vector<int32_t> labels; Tensor out; };
 
 struct Agent {
@@ -422,6 +516,8 @@ struct Oracle {
     std::vector<double> P;                         // S x S mixing matrix
     bool use_current_weights = false;              // planted-mistake switch for tests
     bool storage_bf16 = false;                     // round at the storage points listed above
+    Distill distill;                               // top > 0: the loss is distill_loss
+    std::vector<int32_t> ids; std::vector<double> teacher;       // of the next step's batch
     long t = 0;
     std::vector<std::vector<Agent>> ag;            // [s][k]
     std::vector<size_t> poff;                      // parameter offset of module k in the full vector
@@ -444,6 +540,7 @@ std::vector<double> pass_weights(const Oracle& o, int p, int q, const std::vecto
         size_t nmat = 0;
         if (Y.kind == LINEAR || Y.kind == CONV1X1) nmat = (size_t)Y.c_in * Y.c_out;
         else if (Y.kind == CONV3X3) nmat = (size_t)9 * Y.c_in * Y.c_out;
+        else if (Y.kind == EMBEDDING) nmat = (size_t)Y.c_in * Y.c_out;
         else if (Y.kind == RES_ADD && (Y.flags & 1)) nmat = (size_t)Y.c_in * Y.c_out;
         for (size_t i = 0; i < nmat; ++i) c[off + i] = round_bf16(c[off + i]);
         off += layer_param_count(Y);
@@ -488,6 +585,13 @@ int orc_threads() { return num_threads(); }
 size_t orc_param_count(void* h) { return ((Oracle*)h)->poff.back(); }
 void orc_set_flag_use_current_weights(void* h, int on) { ((Oracle*)h)->use_current_weights = on != 0; }
 void orc_set_storage_bf16(void* h, int on) { ((Oracle*)h)->storage_bf16 = on != 0; }
+void orc_set_distill(void* h, int top, double tau, double weight) { ((Oracle*)h)->distill = Distill{top, tau, weight}; }
+// teacher entries [S*B][top] of the batch that the next orc_step brings
+void orc_set_teacher(void* h, const int32_t* ids, const double* teacher) {
+    Oracle& o = *(Oracle*)h;
+    const size_t n = (size_t)o.S * o.B * o.distill.top;
+    o.ids.assign(ids, ids + n); o.teacher.assign(teacher, teacher + n);
+}
 void orc_round_bf16(const double* in, double* out, size_t n) { for (size_t i = 0; i < n; ++i) out[i] = round_bf16(in[i]); }
 
 // worker < 0: set every replica to the same vector.
@@ -528,6 +632,11 @@ int orc_step(void* h, const double* inputs, const int32_t* labels, double eta, d
         Message m; m.batch = o.t; m.t = Tensor(B, o.in_h, o.in_w, o.in_c);
         std::copy(inputs + (size_t)s * B * in_per, inputs + (size_t)(s + 1) * B * in_per, m.t.v.begin());
         m.labels.assign(labels + (size_t)s * B, labels + (size_t)(s + 1) * B);
+        const size_t top = o.distill.top;
+        if (top) {
+            m.ids.assign(o.ids.begin() + s * B * top, o.ids.begin() + (s + 1) * B * top);
+            m.teacher.assign(o.teacher.begin() + s * B * top, o.teacher.begin() + (s + 1) * B * top);
+        }
         o.ag[s][0].act_in = std::move(m);
 
         for (int k = 0; k < K; ++k) {
@@ -540,10 +649,11 @@ int orc_step(void* h, const double* inputs, const int32_t* labels, double eta, d
                 Tensor out = group_forward(o.layers, p, q, e.w.data(), a.act_in.t, &e.sv, o.storage_bf16);
                 if (s == 0) o.tr_fwd[k] = a.act_in.batch;
                 if (k + 1 < K) {                       // send h_{q_k} to (s,k+1): it is read at t+1
-                    Message nx; nx.batch = a.act_in.batch; nx.t = out; nx.labels = a.act_in.labels;
+                    Message nx; nx.batch = a.act_in.batch; nx.t = out; nx.labels = a.act_in.labels; nx.ids = a.act_in.ids; nx.teacher = a.act_in.teacher;
                     o.ag[s][k + 1].act_next = std::move(nx);
                 } else {                               // last module: evaluate phi and its gradient
-                    loss_sum += softmax_ce(out, e.labels.data(), o.scale, &gout);
+                    loss_sum += o.distill.top ? distill_loss(out, e.labels.data(), a.act_in.ids.data(), a.act_in.teacher.data(), o.distill, o.scale, &gout)
+                                              : softmax_ce(out, e.labels.data(), o.scale, &gout);
                     store(gout, o.storage_bf16);
                     loss_batch = a.act_in.batch; bwd_batch = a.act_in.batch;
                 }

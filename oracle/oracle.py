@@ -42,6 +42,8 @@ def lib():
         L.orc_set_flag_use_current_weights.argtypes = [C.c_void_p, C.c_int]
         L.orc_set_storage_bf16.argtypes = [C.c_void_p, C.c_int]
         L.orc_round_bf16.argtypes = [dp, dp, C.c_size_t]
+        L.orc_set_distill.argtypes = [C.c_void_p, C.c_int, C.c_double, C.c_double]
+        L.orc_set_teacher.argtypes = [C.c_void_p, ip, dp]
         L.orc_set_params.argtypes = [C.c_void_p, C.c_int, dp]
         L.orc_get_params.argtypes = [C.c_void_p, C.c_int, dp]
         L.orc_get_grads.argtypes = [C.c_void_p, C.c_int, dp]
@@ -133,10 +135,19 @@ class Oracle:
         """Round every tensor the bf16 configurations store in bf16 (see the C++ header comment)."""
         lib().orc_set_storage_bf16(self.h, int(on))
 
-    def step(self, inputs, labels, lr):
+    def set_distill(self, top: int, tau: float, weight: float):
+        """The loss distils `top` entries of a teacher, given to every step."""
+        self.top = int(top)
+        lib().orc_set_distill(self.h, self.top, float(tau), float(weight))
+
+    def step(self, inputs, labels, lr, ids=None, teacher=None):
         x = np.ascontiguousarray(inputs, dtype=np.float64)
         y = np.ascontiguousarray(labels, dtype=np.int32)
         assert x.size == self.S * self.B * int(np.prod(self.in_shape)) and y.size == self.S * self.B
+        if ids is not None:
+            i, l = np.ascontiguousarray(ids, dtype=np.int32), np.ascontiguousarray(teacher, dtype=np.float64)
+            assert i.size == l.size == self.S * self.B * self.top
+            lib().orc_set_teacher(self.h, _i(i), _d(l))
         loss = C.c_double()
         lb = C.c_int64()
         lib().orc_step(self.h, _d(x), _i(y), float(lr), C.byref(loss), C.byref(lb))

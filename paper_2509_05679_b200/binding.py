@@ -20,7 +20,7 @@ STATUS = {0: "FDG_OK", 1: "FDG_ERR_INVALID_ARG", 2: "FDG_ERR_BAD_SPLIT", 3: "FDG
           4: "FDG_ERR_ARCH", 5: "FDG_ERR_OOM", 6: "FDG_ERR_CUDA", 7: "FDG_ERR_TIMEOUT", 8: "FDG_ERR_STATE"}
 
 EXPORTS = ["fdg_create", "fdg_grid_sms", "fdg_param_count", "fdg_param_layout", "fdg_set_params", "fdg_set_params_worker", "fdg_params_worker",
-           "fdg_grads_worker", "fdg_consensus_error", "fdg_step", "fdg_step_host", "fdg_wait_ingest", "fdg_join", "fdg_params",
+           "fdg_grads_worker", "fdg_consensus_error", "fdg_step", "fdg_step_host", "fdg_set_distill", "fdg_step_distill", "fdg_wait_ingest", "fdg_join", "fdg_params",
            "fdg_grads", "fdg_trace", "fdg_set_lr", "fdg_stats", "fdg_module_times", "fdg_profile", "fdg_profile_read",
            "fdg_bias_grad_static", "fdg_static_last_error",
            "fdg_embedding_forward", "fdg_embedding_workspace", "fdg_embedding_backward", "fdg_recurrence_saved", "fdg_recurrence_forward",
@@ -109,6 +109,10 @@ def lib():
         for name in ("fdg_step", "fdg_step_host"):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = [vp, vp, vp, fp]
+        L.fdg_set_distill.restype = C.c_int
+        L.fdg_set_distill.argtypes = [vp, C.c_int32, C.c_float, C.c_float]
+        L.fdg_step_distill.restype = C.c_int
+        L.fdg_step_distill.argtypes = [vp, vp, vp, vp, vp, fp]
         for name in ("fdg_params", "fdg_grads"):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = [vp, fp, C.c_size_t, C.POINTER(C.c_size_t)]
@@ -290,6 +294,16 @@ class Context:
         self._ck(lib().fdg_step_host(self.h, _ptr(host_inputs), _ptr(host_labels), C.byref(loss) if want_loss else None))
         return loss.value if want_loss else None
 
+    def set_distill(self, top: int, temperature: float = 1.0, weight: float = 1.0):
+        """Before the first step: the loss distils a teacher (fdg_set_distill); steps are then step_distill's."""
+        self._ck(lib().fdg_set_distill(self.h, int(top), float(temperature), float(weight)))
+
+    def step_distill(self, inputs, labels, ids, teacher, want_loss: bool = False) -> Optional[float]:
+        """A step with the teacher's entries: ids int32 [M, top], teacher fp32 [M, top]; device or pinned host buffers."""
+        loss = C.c_float()
+        self._ck(lib().fdg_step_distill(self.h, _ptr(inputs), _ptr(labels), _ptr(ids), _ptr(teacher), C.byref(loss) if want_loss else None))
+        return loss.value if want_loss else None
+
     def wait_ingest(self):
         self._ck(lib().fdg_wait_ingest(self.h))
 
@@ -350,8 +364,12 @@ def bias_grad_static(dev_dy, dtype: str, rows: int, channels: int, dev_db, strea
 
 
 def to_device(net_dtype: str, x: np.ndarray):
-    """Copy a host fp32 batch to the device in the context's storage dtype (plumbing for callers)."""
+    """Copy a host fp32 batch to the device in the context's storage dtype, token ids (int32) as they are (plumbing for callers)."""
     import torch
+    if x.dtype == np.int32:
+        t = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+        torch.cuda.current_stream().synchronize()
+        return t
     t = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda()
     t = t.to(torch.bfloat16).contiguous() if net_dtype == "bf16" else t
     torch.cuda.current_stream().synchronize()      # the library's streams do not wait for torch's

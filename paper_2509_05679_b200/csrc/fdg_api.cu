@@ -21,6 +21,7 @@
 #include "../../include/fdg.h"
 #include "kernels.h"
 #include "launch.h"
+#include "seqops.h"
 #include "tc_gemm.h"
 
 #include <atomic>
@@ -39,7 +40,7 @@ namespace {
 
 thread_local std::string g_create_error;
 
-enum OpType { OP_CONV, OP_BN, OP_RELU, OP_POOL, OP_GAP, OP_ADD };
+enum OpType { OP_CONV, OP_BN, OP_RELU, OP_POOL, OP_GAP, OP_ADD, OP_EMBED, OP_RECUR };
 enum Loc { LOC_IN, LOC_STASH, LOC_NEXT, LOC_LOGITS };
 
 struct TensorDesc {
@@ -48,6 +49,7 @@ struct TensorDesc {
     size_t off;        // byte offset inside a stash slot (LOC_STASH)
     size_t goff;       // byte offset of its gradient inside the module's gradient pool
     bool own_grad;     // gradient lives in the pool (false: d2 slot / dlogits / none)
+    bool ids;          // token ids (int32), the input of a network that begins with an embedding
     size_t elems() const { return (size_t)h * w * c; }
 };
 
@@ -61,6 +63,7 @@ struct Op {
     size_t stats_off;              // byte offset of saved (mean, invstd) inside the stash slot (OP_BN)
     bool acc_in, acc_in2;          // backward accumulates into an already written gradient
     bool need_dgrad;
+    float scale;                                             // OP_EMBED (g.C rows of g.Co channels)
     // tensor-core plan (bf16 storage, channel counts that are multiples of 64, power-of-two images)
     bool tc;
     bool stem;                                               // thin first-layer conv: dedicated FMA kernels
@@ -110,8 +113,9 @@ struct Module {
     size_t n_big, n_small;         // padded element counts of the two parameter segments
     size_t in_elems;               // per-sample elements of the input / output tensor
     size_t stash_slot_bytes, wslot_bytes, grad_pool_bytes, in_slot_bytes;
-    size_t ws_elems, scratch_elems, red_elems;
-    char *in_ring, *stash, *gradpool, *d2, *wring, *wtring;
+    size_t ws_elems, scratch_elems, red_elems, embed_bytes;
+    bool whole;                    // has a layer that runs over all workers at once
+    char *in_ring, *stash, *gradpool, *d2, *wring, *wtring, *embed_ws;
     float *master, *grad, *ws, *lin_ws, *scratch, *red, *cstat[2], *bstat;
     size_t lin_elems;
     size_t pack_bytes[2];          // [0] forward, [1] backward: the weights of the convolutions that mconv.cu takes, per replica, as their kernels read them,
@@ -152,6 +156,10 @@ struct fdg_ctx {
     std::vector<double> P;         // R x R mixing matrix (row-major) when R > 1
     float* P_dev;
     int in_h, in_w, in_c, device;
+    int in_esz;                    // bytes of an input element: 4 for token ids
+    // fdg_set_distill: entries per sample (0: the loss is the labels'), rings like the labels', the losses of a batch's samples
+    int top; float temperature, distill_weight;
+    int32_t* teacher_ids; float *teacher, *losses;
     float lr;
     int64_t t;
     bool have_params;
@@ -316,6 +324,8 @@ std::string compile_module(fdg_ctx* ctx, Module& m, int& h, int& w, int& c, bool
     auto add_tensor = [&](int th, int tw, int tc) { TensorDesc d{}; d.h = th; d.w = tw; d.c = tc; d.loc = LOC_STASH; d.own_grad = true; m.t.push_back(d); return (int)m.t.size() - 1; };
     int cur = add_tensor(h, w, c);
     m.t[0].loc = LOC_IN;
+    m.t[0].ids = m.p == 0 && L[0].kind == FDG_EMBEDDING;
+    m.whole = false;
     m.in_elems = m.t[0].elems();
     std::vector<int> stack;
     size_t big = 0, small = 0;
@@ -445,6 +455,24 @@ std::string compile_module(fdg_ctx* ctx, Module& m, int& h, int& w, int& c, bool
                 if ((tc.h | tc.w) & 1) return "max-pool needs even height and width";
                 Op o{}; o.type = OP_POOL; o.in = cur; o.in2 = -1; o.out = add_tensor(tc.h / 2, tc.w / 2, tc.c); m.ops.push_back(o); cur = o.out; break; }
             case FDG_GLOBAL_AVGPOOL: { Op o{}; o.type = OP_GAP; o.in = cur; o.in2 = -1; o.out = add_tensor(1, 1, tc.c); m.ops.push_back(o); cur = o.out; break; }
+            case FDG_EMBEDDING: {
+                if (l != 0) return "an embedding can only be the network's first layer";
+                if (tc.c != 1) return "an embedding reads ids: in_c must be 1";
+                if (Y.c_in < 1 || Y.c_out < 1 || Y.c_out > 1 << 20) return "embedding sizes must be positive, at most 2^20 channels";
+                if ((double)ctx->M * tc.h * tc.w > 1 << 30) return "more than 2^30 token ids in a step";
+                Op o{}; o.type = OP_EMBED; o.in = cur; o.in2 = -1;
+                o.g = ConvGeom{}; o.g.C = Y.c_in; o.g.Co = Y.c_out;
+                o.scale = Y.flags & 1 ? std::sqrt((float)Y.c_out) : 1.f;
+                o.w_off = seg((size_t)Y.c_in * Y.c_out, true);
+                o.out = add_tensor(tc.h, tc.w, Y.c_out);
+                m.whole = true;
+                m.ops.push_back(o); cur = o.out; break; }
+            case FDG_RECURRENCE: {
+                if (Y.c_out < 1 || Y.c_in != 2 * Y.c_out || Y.c_in != tc.c) return "a recurrence has twice as many input channels (gates, then values) as output channels";
+                if ((double)tc.h * tc.w > 1 << 30) return "more than 2^30 positions";
+                Op o{}; o.type = OP_RECUR; o.in = cur; o.in2 = -1; o.out = add_tensor(tc.h, tc.w, Y.c_out);
+                m.whole = true;
+                m.ops.push_back(o); cur = o.out; break; }
             case FDG_RES_BEGIN: stack.push_back(cur); break;
             case FDG_RES_ADD: {
                 if (stack.empty()) return "RES_ADD without RES_BEGIN";
@@ -486,8 +514,10 @@ std::string compile_module(fdg_ctx* ctx, Module& m, int& h, int& w, int& c, bool
         if (d.own_grad) { d.goff = goff; goff += align_up(d.elems() * ctx->M * ctx->esz, 256); }
     }
     size_t red_pos = 0;
-    m.ws_elems = 0; m.scratch_elems = 64; m.red_elems = 4; m.lin_elems = 0;
+    m.ws_elems = 0; m.scratch_elems = 64; m.red_elems = 4; m.lin_elems = 0; m.embed_bytes = 0;
     for (Op& o : m.ops) {
+        if (o.type == OP_EMBED) m.embed_bytes = embed_workspace_bytes((long)(ctx->R > 1 ? ctx->B : ctx->M) * m.t[o.in].h * m.t[o.in].w, o.g.C, o.g.Co);
+        if (o.type == OP_RECUR) { o.stats_off = soff; soff += align_up(recur_saved_bytes(ctx->dt, ctx->M, m.t[o.in].h * m.t[o.in].w, m.t[o.out].c), 256); }
         if (o.type == OP_BN) {
             o.stats_off = soff; soff += align_up((size_t)ctx->n_workers * o.g.C * (ctx->dt == 0 ? 4 : 2) * sizeof(float), 256);
             m.scratch_elems = std::max(m.scratch_elems, (size_t)128 * ctx->n_workers * o.g.C * 2);
@@ -683,7 +713,7 @@ bool tc_stem_wgrad(fdg_ctx* c, Module& m, const Op& o, char* x_base, char* dy_ba
 
 // byte offset of the group's first sample inside a tensor of the module
 size_t row_off(const fdg_ctx* c, const TensorDesc& d, const Win& wn) {
-    return (size_t)wn.n0 * d.elems() * (d.loc == LOC_LOGITS ? sizeof(float) : (size_t)c->esz);
+    return (size_t)wn.n0 * d.elems() * (d.loc == LOC_LOGITS || d.ids ? 4 : (size_t)c->esz);
 }
 
 // The weights of version `version` for one pass of the convolutions in mconv.cu: one launch for all of a module's (up to PackArgs::MAX).
@@ -699,6 +729,17 @@ Packed packed(const Module& m, const Op& o, bool back, int rep) {
 }
 // all groups of a launch read the same weights
 Packed shared(Packed p) { p.group = 0; return p; }
+
+// A recurrence on all samples: gates and values are the halves of a position's channels.
+RecurArgs recur_args(const fdg_ctx* c, const Op& o, const TensorDesc& ti, const TensorDesc& to, const StepPtrs& P) {
+    RecurArgs a{};
+    a.B = c->M; a.T = (long)ti.h * ti.w; a.C = to.c;
+    a.z = P.tensor(o.in); a.v = P.tensor(o.in) + (size_t)to.c * c->esz;
+    a.z_t = a.v_t = ti.c; a.z_b = a.v_b = a.T * ti.c;
+    a.y = P.tensor(o.out); a.y_t = to.c; a.y_b = a.T * to.c;
+    a.saved = P.stats(o);
+    return a;
+}
 
 // The ops [i0, i1) of a module's forward pass on one group's rows.
 void forward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int group, size_t i0, size_t i1) {
@@ -719,7 +760,7 @@ void forward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int group, 
                 int epi = (o.relu ? EPI_RELU : 0) | (to.loc == LOC_LOGITS ? EPI_OUT_F32 : 0);
                 ConvGeom g = o.g; g.N = wn.n;
                 profile_detail(o.shape);
-                if (o.head && m.groups == 1) {
+                if (o.head && m.groups == 1 && !c->top) {
                     // logits, parts of the loss and dphi/dlogits / M of batch `batch` in one launch; the backward pass of the same iteration adds the parts
                     head_forward_loss(dt, T(o.in), wbig(c, m, version, o.w_off), o.bias ? wsmall(c, m, version, o.b_off) : nullptr,
                                       c->labels + (size_t)(batch % c->label_depth) * c->M, c->logits, c->dlogits, m.head_scratch + m.head_part_elems,
@@ -782,6 +823,10 @@ void forward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int group, 
             case OP_POOL: maxpool_forward(dt, T(o.in), T(o.out), wn.n, ti.h, ti.w, ti.c, s); break;
             case OP_GAP: gap_forward(dt, T(o.in), T(o.out), wn.n, ti.h * ti.w, ti.c, s); break;
             case OP_ADD: add_forward(dt, T(o.in), T(o.in2), T(o.out), n_out, s); break;
+            case OP_EMBED:
+                embed_forward(dt, (const int32_t*)T(o.in), (long)wn.n * ti.h * ti.w, wbig(c, m, version, o.w_off, rep), o.g.C, o.g.Co, o.scale, T(o.out), o.g.Co, s);
+                break;
+            case OP_RECUR: recur_forward(dt, recur_args(c, o, ti, to, P), s); break;
         }
     }
 }
@@ -829,6 +874,8 @@ bool forward_op_replicas(fdg_ctx* c, int kk, int64_t batch, int64_t version, siz
         case OP_POOL: maxpool_forward(dt, P.tensor(o.in), P.tensor(o.out), c->M, ti.h, ti.w, ti.c, s); return true;
         case OP_GAP: gap_forward(dt, P.tensor(o.in), P.tensor(o.out), c->M, ti.h * ti.w, ti.c, s); return true;
         case OP_ADD: add_forward(dt, P.tensor(o.in), P.tensor(o.in2), P.tensor(o.out), to.elems() * c->M, s); return true;
+        case OP_EMBED: return false;
+        case OP_RECUR: recur_forward(dt, recur_args(c, o, ti, to, P), s); return true;
     }
     return false;
 }
@@ -859,6 +906,16 @@ char* grad_ptr(fdg_ctx* c, int kk, int id, int64_t t) {
     return n.d2 + (size_t)((t - 1) & 1) * n.in_slot_bytes;
 }
 
+// Gradients of a recurrence, gin: those of its input (not the network's, which nobody wants).
+void recur_back(fdg_ctx* c, const Op& o, const TensorDesc& ti, const TensorDesc& to, const StepPtrs& P, const char* gout, char* gin, cudaStream_t s) {
+    RecurArgs a = recur_args(c, o, ti, to, P);
+    a.dy = gout; a.dy_t = to.c; a.dy_b = a.T * to.c;
+    a.dz = gin; a.dv = gin + (size_t)to.c * c->esz;
+    a.dz_t = a.dv_t = ti.c; a.dz_b = a.dv_b = a.T * ti.c;
+    a.accum = o.acc_in;
+    recur_backward(c->dt, a, s);
+}
+
 // The ops i1 - 1 down to i0 of a module's backward pass on one group's rows.
 void backward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int64_t t, int group, int i0, int i1) {
     Module& m = c->mod[kk];
@@ -885,7 +942,7 @@ void backward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int64_t t,
         switch (o.type) {
             case OP_CONV: {
                 ConvGeom g = o.g; g.N = wn.n;
-                if (o.head && m.groups == 1) {
+                if (o.head && m.groups == 1 && !c->top) {
                     profile_detail(o.shape);
                     head_backward(dt, T(o.in), wbig(c, m, version, o.w_off), gout, gin, o.acc_in, o.masks > 0, col, m.head_scratch, c->M, g.C, g.Co, s);
                     cudaStream_t ws = m.wstream;                     // the sum of the partials is needed by the update only
@@ -964,6 +1021,12 @@ void backward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int64_t t,
                 char* g2 = G(o.in2);
                 if (g2) copy_or_accumulate(dt, gout, g2, n_in, o.acc_in2, s);
                 break; }
+            case OP_EMBED: {                                         // needed by the update only, as the weight gradients are
+                cudaStream_t ws = m.wstream;
+                if (ws != s) { step_record(m.wev, s); step_wait(ws, m.wev); }
+                embed_backward(dt, (const int32_t*)T(o.in), (long)wn.n * ti.h * ti.w, gout, o.g.Co, o.g.C, o.g.Co, o.scale, acc_p, mgrad + o.w_off, m.embed_ws, ws);
+                break; }
+            case OP_RECUR: if (gin) recur_back(c, o, ti, to, P, gout, gin, s); break;
         }
     }
 }
@@ -1012,6 +1075,8 @@ bool backward_op_replicas(fdg_ctx* c, int kk, int64_t batch, int64_t version, in
             if (gin) copy_or_accumulate(dt, gout, gin, n_in, o.acc_in, s);
             if (char* g2 = grad_ptr(c, kk, o.in2, t)) copy_or_accumulate(dt, gout, g2, n_in, o.acc_in2, s);
             return true; }
+        case OP_EMBED: return false;
+        case OP_RECUR: if (gin) recur_back(c, o, ti, m.t[o.out], P, gout, gin, s); return true;
     }
     return false;
 }
@@ -1234,7 +1299,7 @@ fdg_status module_step(fdg_ctx* ctx, int kk, int64_t t, const Ingest* in, int pa
     const int64_t v_b = tau_b + kk;                       // t - 2K + 2k: the version the forward of tau_b used
     const bool lastm = kk == K - 1;
     if (in && (part & FORWARD)) {
-        ingest(in->x, m.in_ring + (size_t)(t % m.in_depth) * m.in_slot_bytes, (size_t)ctx->M * m.in_elems * ctx->esz, in->y,
+        ingest(in->x, m.in_ring + (size_t)(t % m.in_depth) * m.in_slot_bytes, (size_t)ctx->M * m.in_elems * ctx->in_esz, in->y,
                ctx->labels + (size_t)(t % ctx->label_depth) * ctx->M, ctx->M, m.fstream);
         // inside a graph: an event the host can wait for
         if (StepGraph* g = StepGraph::current()) { if (g->mode() == StepGraph::CAPTURE) CK(cudaEventRecordWithFlags(ctx->ingested, m.fstream, cudaEventRecordExternal)); }
@@ -1272,8 +1337,19 @@ fdg_status module_step(fdg_ctx* ctx, int kk, int64_t t, const Ingest* in, int pa
         LossRecord* const rec = ctx->loss_ring + (t % 64);
         // one replica: dphi/dlogits / M, the mean over all samples.  One replica per worker: / B, worker s's own
         // gradient scale 1/per_worker_batch of Eq. dl_update (the mixing matrix does the averaging)
-        const bool fused_head = m.ops.back().head && m.groups == 1;     // the forward pass above has computed loss and dlogits
+        const bool fused_head = m.ops.back().head && m.groups == 1 && !ctx->top;     // the forward pass above has computed loss and dlogits
         if (tau_f < 0) publish_loss_value(rec, NAN, ctx->tc_err, t + 1, m.stream);
+        else if (ctx->top) {
+            const size_t slot = (size_t)(tau_f % ctx->label_depth) * ctx->M;
+            DistillArgs a{};
+            a.M = ctx->M; a.V = ctx->classes; a.k = ctx->top;
+            a.logits = ctx->logits; a.logits_stride = ctx->classes; a.labels = ctx->labels + slot;
+            a.ids = ctx->teacher_ids + slot * ctx->top; a.teacher = ctx->teacher + slot * ctx->top;
+            a.tau = ctx->temperature; a.weight = ctx->distill_weight; a.scale = ctx->R > 1 ? 1.f / (float)ctx->B : 1.f / (float)ctx->M;
+            a.loss = ctx->losses; a.grad = ctx->dlogits; a.grad_stride = ctx->classes;
+            distill(0, ctx->dt, a, m.stream);
+            publish_loss_mean(rec, ctx->losses, ctx->M, ctx->tc_err, t + 1, m.stream);
+        }
         else if (!fused_head) softmax_ce(ctx->dt, ctx->logits, ctx->labels + (size_t)(tau_f % ctx->label_depth) * ctx->M, ctx->dlogits, rec, ctx->tc_err, t + 1,
                                          ctx->M, ctx->classes, ctx->R > 1 ? 1.f / (float)ctx->B : 1.f / (float)ctx->M, m.stream);
     }
@@ -1357,18 +1433,28 @@ fdg_status wait_loss(fdg_ctx* ctx, const LossRecord* rec, int64_t seq, float* lo
     return FDG_OK;
 }
 
-fdg_status run_step(fdg_ctx* ctx, const void* inputs, const int32_t* labels, bool host_src, float* host_loss) {
+struct Teacher { const int32_t* ids; const float* logits; };
+
+fdg_status run_step(fdg_ctx* ctx, const void* inputs, const int32_t* labels, const Teacher* teacher, bool host_src, float* host_loss) {
     if (!ctx) return FDG_ERR_INVALID_ARG;
     if (!inputs || !labels) return fail(ctx, FDG_ERR_INVALID_ARG, "inputs and labels must not be NULL");
+    if (teacher && (!teacher->ids || !teacher->logits)) return fail(ctx, FDG_ERR_INVALID_ARG, "ids and teacher must not be NULL");
+    if (!teacher != !ctx->top) return fail(ctx, FDG_ERR_STATE, teacher ? "fdg_set_distill must be called before fdg_step_distill" : "this context distils: its steps are fdg_step_distill's");
     if (!ctx->have_params) return fail(ctx, FDG_ERR_STATE, "fdg_set_params must be called before fdg_step");
     if (ctx->broken) return fail(ctx, FDG_ERR_STATE, "an earlier step failed after part of its work was enqueued; call fdg_set_params to start over");
-    const size_t x_bytes = (size_t)ctx->M * ctx->mod[0].in_elems * ctx->esz, y_bytes = (size_t)ctx->M * sizeof(int32_t);
+    const size_t x_bytes = (size_t)ctx->M * ctx->mod[0].in_elems * ctx->in_esz, y_bytes = (size_t)ctx->M * sizeof(int32_t);
     bool by_copy = host_src;
     if (!host_src) {
-        const Readable x = readable(ctx, inputs, x_bytes, 2), y = readable(ctx, labels, y_bytes, 4);
+        const Readable x = readable(ctx, inputs, x_bytes, ctx->mod[0].t[0].ids ? 4 : 2), y = readable(ctx, labels, y_bytes, 4);
         if (x == NOT_READABLE || y == NOT_READABLE)
             return fail(ctx, FDG_ERR_INVALID_ARG, "%s must be device memory of %zu bytes", x == NOT_READABLE ? "inputs" : "labels", x == NOT_READABLE ? x_bytes : y_bytes);
         by_copy = x == BY_COPY || y == BY_COPY;
+    }
+    const size_t k_bytes = (size_t)ctx->M * ctx->top * 4;
+    if (teacher) {
+        const Readable i = readable(ctx, teacher->ids, k_bytes, 4), l = readable(ctx, teacher->logits, k_bytes, 4);
+        if (i == NOT_READABLE || l == NOT_READABLE) return fail(ctx, FDG_ERR_INVALID_ARG, "%s must be device or pinned memory of %zu bytes", i == NOT_READABLE ? "ids" : "teacher", k_bytes);
+        by_copy = true;
     }
     const int K = ctx->K;
     const int64_t t = ctx->t;
@@ -1405,6 +1491,11 @@ fdg_status run_step(fdg_ctx* ctx, const void* inputs, const int32_t* labels, boo
         if (ahead && t > 1) CK(cudaStreamWaitEvent(copy, m0.done[now], 0));                  // iteration t-2 (this iteration's record comes later)
         CK(cudaMemcpyAsync(m0.in_ring + (size_t)(t % m0.in_depth) * m0.in_slot_bytes, inputs, x_bytes, kind, copy));
         CK(cudaMemcpyAsync(ctx->labels + (size_t)(t % ctx->label_depth) * ctx->M, labels, y_bytes, kind, copy));
+        if (teacher) {
+            const size_t slot = (size_t)(t % ctx->label_depth) * ctx->M * ctx->top;
+            CK(cudaMemcpyAsync(ctx->teacher_ids + slot, teacher->ids, k_bytes, kind, copy));
+            CK(cudaMemcpyAsync(ctx->teacher + slot, teacher->logits, k_bytes, kind, copy));
+        }
         CK(cudaEventRecord(ctx->ingested, copy));
         CK(cudaStreamWaitEvent(as_graph(m0, 0) && !m0.split ? m0.stream : m0.fstream, ctx->ingested, 0));
         // the last module reads the labels: K - 1 iterations from now, ordered by the hand-offs; with one module in this iteration's forward pass
@@ -1519,6 +1610,8 @@ fdg_status fdg_create(const fdg_layer* layers, int32_t n_layers, const int32_t* 
     }
     ctx->in_h = opt->in_h; ctx->in_w = opt->in_w; ctx->in_c = opt->in_c; ctx->lr = lr; ctx->t = 0; ctx->have_params = false; ctx->broken = false;
     ctx->layers.assign(layers, layers + n_layers);
+    ctx->in_esz = layers[0].kind == FDG_EMBEDDING ? 4 : ctx->esz;
+    ctx->top = 0; ctx->teacher_ids = nullptr; ctx->teacher = ctx->losses = nullptr;
     ctx->alloc = alloc ? *alloc : fdg_allocator{default_alloc, default_free, nullptr};
     ctx->own_streams = opt->streams == nullptr;
     ctx->device_bytes = 0;
@@ -1546,13 +1639,13 @@ fdg_status fdg_create(const fdg_layer* layers, int32_t n_layers, const int32_t* 
         // a group is a whole number of workers; the last module of a split network stays whole
         m.groups = 1;
         if (ctx->R > 1) m.groups = n_workers;
-        else if (opt->worker_groups > 1 && (kk + 1 < K || K == 1)) {
+        else if (opt->worker_groups > 1 && !m.whole && (kk + 1 < K || K == 1)) {
             int g = 1;
             while (g * 2 <= opt->worker_groups && n_workers % (g * 2) == 0) g *= 2;
             m.groups = g;
         }
         plan_packs(ctx, m, kk == 0);
-        m.in_slot_bytes = align_up((size_t)ctx->M * m.in_elems * ctx->esz, 256);
+        m.in_slot_bytes = align_up((size_t)ctx->M * m.in_elems * (kk == 0 ? ctx->in_esz : ctx->esz), 256);
         m.wslot_bytes = align_up(m.n_big * ctx->esz + m.n_small * sizeof(float), 256);
     }
     // Two graphs per module (forward / backward + update) let a module's next forward pass start before its neighbours' backward passes are
@@ -1601,6 +1694,7 @@ fdg_status fdg_create(const fdg_layer* layers, int32_t n_layers, const int32_t* 
         m.master = (float*)get((size_t)ctx->R * (m.n_big + m.n_small) * sizeof(float));
         m.grad = (float*)get((size_t)ctx->R * (m.n_big + m.n_small) * sizeof(float));
         m.ws = (float*)get(m.ws_elems * sizeof(float));
+        m.embed_ws = m.embed_bytes ? get(m.embed_bytes) : nullptr;
         m.lin_ws = m.lin_elems ? (float*)get(m.lin_elems * sizeof(float)) : nullptr;
         for (int back = 0; back < 2; ++back) m.pack[back] = m.pack_bytes[back] ? get(m.pack_bytes[back] * ctx->R) : nullptr;
         m.scratch = (float*)get(m.scratch_elems * sizeof(float));
@@ -1761,6 +1855,7 @@ fdg_status fdg_param_layout(const fdg_ctx* ctx, fdg_param_tensor* out, int32_t c
                 emit(l, FDG_PARAM_W, 4, Y.c_out, r, r, Y.c_in);
                 if (Y.flags & 1) emit(l, FDG_PARAM_BIAS, 1, Y.c_out, 1, 1, 1);
                 break; }
+            case FDG_EMBEDDING: emit(l, FDG_PARAM_W, 2, Y.c_in, Y.c_out, 1, 1); break;
             case FDG_BATCHNORM:
                 emit(l, FDG_PARAM_GAMMA, 1, Y.c_in, 1, 1, 1);
                 emit(l, FDG_PARAM_BETA, 1, Y.c_in, 1, 1, 1);
@@ -1831,16 +1926,42 @@ fdg_status fdg_set_params_worker(fdg_ctx* ctx, int32_t worker, const float* host
 
 // A CUDA error in the middle of a step leaves some of its kernels enqueued and the iteration counter where it was:
 // the context then refuses further steps until fdg_set_params resets the FIFOs.
-static fdg_status guarded_step(fdg_ctx* ctx, const void* inputs, const int32_t* labels, bool host_src, float* host_loss) {
-    const fdg_status s = run_step(ctx, inputs, labels, host_src, host_loss);
+static fdg_status guarded_step(fdg_ctx* ctx, const void* inputs, const int32_t* labels, const Teacher* teacher, bool host_src, float* host_loss) {
+    const fdg_status s = run_step(ctx, inputs, labels, teacher, host_src, host_loss);
     if (ctx && (s == FDG_ERR_CUDA || s == FDG_ERR_TIMEOUT)) ctx->broken = true;
     return s;
 }
 fdg_status fdg_step(fdg_ctx* ctx, const void* dev_inputs, const int32_t* dev_labels, float* host_loss_or_null) {
-    return guarded_step(ctx, dev_inputs, dev_labels, false, host_loss_or_null);
+    return guarded_step(ctx, dev_inputs, dev_labels, nullptr, false, host_loss_or_null);
 }
 fdg_status fdg_step_host(fdg_ctx* ctx, const void* host_inputs, const int32_t* host_labels, float* host_loss_or_null) {
-    return guarded_step(ctx, host_inputs, host_labels, true, host_loss_or_null);
+    return guarded_step(ctx, host_inputs, host_labels, nullptr, true, host_loss_or_null);
+}
+fdg_status fdg_step_distill(fdg_ctx* ctx, const void* inputs, const int32_t* labels, const int32_t* ids, const float* teacher, float* host_loss_or_null) {
+    const Teacher t{ids, teacher};
+    return guarded_step(ctx, inputs, labels, &t, false, host_loss_or_null);
+}
+
+fdg_status fdg_set_distill(fdg_ctx* ctx, int32_t top, float temperature, float weight) {
+    if (!ctx) return FDG_ERR_INVALID_ARG;
+    if (top < 1 || top > DISTILL_MAX_TOP) return fail(ctx, FDG_ERR_INVALID_ARG, "top must be 1..%d", DISTILL_MAX_TOP);
+    if (!(temperature >= 1e-6f && temperature <= 1e6f)) return fail(ctx, FDG_ERR_INVALID_ARG, "temperature must be 1e-6..1e6");
+    if (!(weight >= 0.f && weight <= 1.f)) return fail(ctx, FDG_ERR_INVALID_ARG, "weight must be 0..1");
+    if (ctx->classes > DISTILL_MAX_VOCAB) return fail(ctx, FDG_ERR_UNSUPPORTED, "distillation is supported for at most %ld classes", DISTILL_MAX_VOCAB);
+    if (ctx->top) return fail(ctx, FDG_ERR_STATE, "the context distils already");
+    if (ctx->t != 0 || ctx->broken) return fail(ctx, FDG_ERR_STATE, "fdg_set_distill must be called before the first step");
+    const size_t ring = align_up((size_t)ctx->label_depth * ctx->M * top * 4, 256), losses = align_up((size_t)ctx->M * sizeof(float), 256);
+    char* const p = (char*)ctx->alloc.alloc(2 * ring + losses, ctx->alloc.user);
+    if (!p) return fail(ctx, FDG_ERR_OOM, "the allocator returned NULL");
+    ctx->blocks.push_back(p); ctx->device_bytes += 2 * ring + losses;
+    ctx->teacher_ids = (int32_t*)p; ctx->teacher = (float*)(p + ring); ctx->losses = (float*)(p + 2 * ring);
+    ctx->top = top; ctx->temperature = temperature; ctx->distill_weight = weight;
+    // the fused classifier head is off: it masked the error gradient of the layer below, which now does so itself
+    Module& m = ctx->mod[ctx->K - 1];
+    Op& head = m.ops.back();
+    if (head.head && head.masks > 0) { m.ops[head.masks - 1].masked_by = 0; head.masks = 0; }
+    for (Module& q : ctx->mod) { for (StepGraph& g : q.graph) g.clear(); q.ran_direct = false; }      // of an earlier run of this context
+    return FDG_OK;
 }
 
 // worker < 0: the parameters of replica 0, or the gradient averaged over the replicas

@@ -1098,6 +1098,20 @@ void publish_loss_value(LossRecord* rec, float loss, const int* err, long long s
     klaunch(publish_k, 1, 1, 0, s, rec, loss, err, seq);
 }
 
+__global__ void publish_mean_k(LossRecord* rec, const float* __restrict__ losses, int M, const int* err, long long seq) {
+    __shared__ double sh[256];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < M; i += 256) sum += losses[i];
+    sh[threadIdx.x] = sum;
+    __syncthreads();
+    for (int s = 128; s > 0; s >>= 1) { if ((int)threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s]; __syncthreads(); }
+    if (threadIdx.x == 0) publish_loss(rec, (float)(sh[0] / M), err, seq);
+}
+void publish_loss_mean(LossRecord* rec, const float* losses, int M, const int* err, long long seq, cudaStream_t s) {
+    Scope sc(KC_FILL, 0.0, 4.0 * M, s);
+    klaunch(publish_mean_k, 1, 256, 0, s, rec, losses, M, err, seq);
+}
+
 template <typename T>
 __global__ void softmax_ce_k(const float* __restrict__ z, const int32_t* __restrict__ labels, T* __restrict__ dz,
                              LossRecord* rec, const int* err, long long seq, int M, int C, float scale) {

@@ -131,6 +131,8 @@ void bn_backward(int dt, const void* x, const void* out, const void* dout, const
 // Where a step's loss reaches the host: pinned memory the kernel that computes it writes to (seq last).
 struct LossRecord { float loss; int err; long long seq; };
 void publish_loss_value(LossRecord* rec, float loss, const int* err, long long seq, cudaStream_t st);
+// the mean of M samples' losses
+void publish_loss_mean(LossRecord* rec, const float* losses, int M, const int* err, long long seq, cudaStream_t st);
 
 // Softmax cross-entropy over fp32 logits [M, classes]: dlogits (storage dtype) = (softmax - onehot) * scale,
 // rec: the mean loss, the error word `err` and the number `seq`.  Deterministic single-block reduction.

@@ -10,7 +10,7 @@ Layer records are 5 integers ``(kind, c_in, c_out, stride, flags)``.
 Canonical parameter order (both the library and the oracle use it): layers in list order; for
 each layer ``W`` then ``b`` (linear ``W[out][in]``; conv ``W[c_out][kh][kw][c_in]``), batch-norm
 ``gamma`` then ``beta``; a residual add with projection carries ``Wp[c_out][c_in]`` (1x1 conv,
-no bias) followed by the projection batch-norm's ``gamma`` and ``beta``.
+no bias) followed by the projection batch-norm's ``gamma`` and ``beta``; an embedding its table ``W[c_in][c_out]``.
 
 Activations are NHWC, worker-major: rows ``s*B .. (s+1)*B-1`` of a batch belong to worker ``s``.
 """
@@ -22,8 +22,9 @@ from typing import List, Sequence, Tuple
 import numpy as np
 
 # layer kinds (values are part of the C interface)
-LINEAR, CONV3X3, CONV1X1, RELU, MAXPOOL2, GLOBAL_AVGPOOL, BATCHNORM, RES_BEGIN, RES_ADD = range(9)
+LINEAR, CONV3X3, CONV1X1, RELU, MAXPOOL2, GLOBAL_AVGPOOL, BATCHNORM, RES_BEGIN, RES_ADD, EMBEDDING, RECURRENCE = range(11)
 FLAG_BIAS = 1        # LINEAR / CONV*: layer has a bias vector
+FLAG_SCALED = 1      # EMBEDDING: rows times sqrt(c_out)
 FLAG_PROJ = 1        # RES_ADD: shortcut is conv1x1(stride) + batch-norm instead of identity
 
 Layer = Tuple[int, int, int, int, int]
@@ -72,6 +73,8 @@ def param_shapes(layers: Sequence[Layer]) -> List[Tuple[int, str, Tuple[int, ...
             out.append((i, "W", (cout, r, r, cin), r * r * cin))
             if flags & FLAG_BIAS:
                 out.append((i, "b", (cout,), 0))
+        elif kind == EMBEDDING:
+            out.append((i, "W", (cin, cout), 2 * cout))          # rows of norm 1 with the He initialisation below
         elif kind == BATCHNORM:
             out.append((i, "gamma", (cin,), -1))
             out.append((i, "beta", (cin,), 0))
@@ -128,9 +131,21 @@ def perturb_params(params: np.ndarray, layers: Sequence[Layer], seed: int, scale
 
 def batch_inputs(net: Net, t: int, stream: int = 0) -> np.ndarray:
     """Inputs of iteration t: [M, in_h, in_w, in_c] i.i.d. N(0,1), fp32 (bf16-representable
-    when the configuration computes in bf16).  `stream` selects an independent data stream."""
+    when the configuration computes in bf16); of a network that begins with an embedding: int32 ids, one in
+    sixteen of them -1 (padding).  `stream` selects an independent data stream."""
+    if net.layers[0][0] == EMBEDDING:
+        g = _rng(1000 + t + 1000003 * stream)
+        ids = g.integers(0, net.layers[0][1], size=(net.M, net.in_h, net.in_w, 1), dtype=np.int32)
+        return np.where(g.integers(0, 16, size=ids.shape) == 0, np.int32(-1), ids)
     x = _rng(1000 + t + 1000003 * stream).standard_normal((net.M, net.in_h, net.in_w, net.in_c)).astype(np.float32)
     return round_to_bf16(x) if net.dtype == "bf16" else x
+
+
+def batch_teacher(net: Net, t: int, top: int, stream: int = 0):
+    """A teacher's `top` entries for the samples of iteration t: distinct class ids int32 [M, top], logits fp32 [M, top]."""
+    g = _rng(3000 + t + 1000003 * stream)
+    ids = np.argsort(g.random((net.M, net.classes)), axis=1)[:, :top].astype(np.int32)
+    return np.ascontiguousarray(ids), (2 * g.standard_normal((net.M, top))).astype(np.float32)
 
 
 def batch_labels(net: Net, t: int, stream: int = 0) -> np.ndarray:
