@@ -4,12 +4,15 @@
 //   grad_v = scale (w tau (q_v - sum of the p_j with id_j = v) + (1 - w) (q1_v - [v = label]))
 // The logits are read once and the gradient is written once, which is the bound (HBM): a row stays in shared memory between its maximum, its sums and its
 // gradient, cut over a cluster where one CTA's share would keep others from its SM.  The exponentials come close to being a second bound: the special-function
-// unit makes 16 a cycle and SM, and an element needs one for either temperature in either pass.  Where tau is 1, 2, 4 or 8, exp(d) is a power of exp(d / tau).
+// unit makes 16 a cycle and SM, and an element needs one for either temperature in either pass.  Where tau is 1, 2 or 4, exp(d) is a power of exp(d / tau).
 #include "seqops.h"
 #include "launch.h"
 
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
 
 namespace fdg {
 namespace {
@@ -21,7 +24,7 @@ __device__ __forceinline__ float ld(const bf16* p) { return __bfloat162float(*p)
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int THREADS = 256, WARPS = THREADS / 32;             // of distill_warp_k
 constexpr int MAX_CLUSTER = 8;
 
 // Results below 2^-126 are zero: beside the maximum's exponential, which is 1, that is nothing, and subnormal ones cost three instructions more.
@@ -40,6 +43,20 @@ template <typename F> __device__ __forceinline__ float reduce_warp(float v, F f)
 // lead from the first to the second; -1: any tau.
 template <int SQ, bool HARD> struct Exps {
     float c;                                        // log2(e) / tau
+    // two at once, through the packed fp32 instructions
+    __device__ __forceinline__ void operator()(float2 d, float2& et, float2& e1) const {
+        const float2 x = __fmul2_rn(d, make_float2(c, c));
+        et = make_float2(exp2_(x.x), exp2_(x.y));
+        if (!HARD) { e1 = make_float2(0.f, 0.f); return; }
+        if (SQ < 0) {
+            const float2 z = __fmul2_rn(d, make_float2(LOG2E, LOG2E));
+            e1 = make_float2(exp2_(z.x), exp2_(z.y));
+        } else {
+            e1 = et;
+#pragma unroll
+            for (int i = 0; i < SQ; ++i) e1 = __fmul2_rn(e1, e1);
+        }
+    }
     __device__ __forceinline__ void operator()(float d, float& et, float& e1) const {
         et = exp2_(d * c);
         if (!HARD) { e1 = 0.f; return; }
@@ -136,234 +153,310 @@ __global__ void __launch_bounds__(THREADS) distill_warp_k(DistillArgs a) {
 template <typename T> struct Chunk;                 // 16 bytes of logits
 template <> struct Chunk<float> { static constexpr int E = 4; };
 template <> struct Chunk<bf16> { static constexpr int E = 8; };
-__device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) { x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w); }
-__device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+__device__ __forceinline__ void unpack(const uint4& r, float2 (&x)[2]) {
+    x[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y)); x[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
+}
+__device__ __forceinline__ void unpack(const uint4& r, float2 (&x)[4]) {
     const unsigned w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ unsigned pair(float a, float b) { const __nv_bfloat162 v = __floats2bfloat162_rn(a, b); return *(const unsigned*)&v; }
-__device__ __forceinline__ void put(float* p, const float (&x)[4]) { *(float4*)p = make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ void put(bf16* p, const float (&x)[4]) { *(uint2*)p = make_uint2(pair(x[0], x[1]), pair(x[2], x[3])); }
-__device__ __forceinline__ void put(bf16* p, const float (&x)[8]) { *(uint4*)p = make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7])); }
+__device__ __forceinline__ unsigned pair(float2 a) { const __nv_bfloat162 v = __float22bfloat162_rn(a); return *(const unsigned*)&v; }
+__device__ __forceinline__ void put(float* p, const float2 (&x)[2]) { *(float4*)p = make_float4(x[0].x, x[0].y, x[1].x, x[1].y); }
+__device__ __forceinline__ void put(bf16* p, const float2 (&x)[2]) { *(uint2*)p = make_uint2(pair(x[0]), pair(x[1])); }
+__device__ __forceinline__ void put(bf16* p, const float2 (&x)[4]) { *(uint4*)p = make_uint4(pair(x[0]), pair(x[1]), pair(x[2]), pair(x[3])); }
+// the largest values so far: of a chunk's words, and both halves' in the end (a NaN comes back by way of the sums)
+struct Top {
+    float m = -INFINITY;
+    __nv_bfloat162 m2 = __float2bfloat162_rn(-INFINITY);
+    __device__ __forceinline__ void add(const uint4& r, float) {
+        m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(r.x), __uint_as_float(r.y))), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+    }
+    __device__ __forceinline__ void add(const uint4& r, bf16) {
+        const __nv_bfloat162* const v = (const __nv_bfloat162*)&r;
+        m2 = __hmax2(__hmax2(m2, __hmax2(v[0], v[1])), __hmax2(v[2], v[3]));
+    }
+    __device__ __forceinline__ float value() const { return fmaxf(m, fmaxf(__low2float(m2), __high2float(m2))); }
+};
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void copy16(void* smem, const void* g) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(smem)), "l"(g) : "memory");
 }
 template <int LEFT> __device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-constexpr int PARTS = 4;                            // of a row's copies, so that the maximum of the first begins while the last are on their way
+__device__ __forceinline__ void copy4(void* smem, const void* g) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((unsigned)__cvta_generic_to_shared(smem)), "l"(g) : "memory");
+}
 
 // A row is cut into chunks of 16 aligned bytes, the first and the last one partly outside the row (there: -infinity).  A thread copies, and in every pass
-// handles, the chunks threadIdx.x, + THREADS, ... of its CTA's share.
-template <typename TI, typename TO, int SQ, bool HARD, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 3) distill_row_k(DistillArgs a, int ranks, int share) {
-    constexpr int E = Chunk<TI>::E;
+// handles, the chunks threadIdx.x, + THREADS, ... of its CTA's share, so that it can have the next row's chunk copied to where it has just read this one's for the last
+// time: a CTA (or cluster) goes through the rows row0, + step, ... with the next row on its way while the gradient of this one is written.
+template <typename TI, typename TO, int SQ, bool HARD, bool CLUSTER, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k(DistillArgs a, int ranks, int share) {
+    constexpr int WARPS = THREADS / 32, E = Chunk<TI>::E;
     extern __shared__ __align__(16) char dyn[];
     uint4* const chunks = (uint4*)dyn;
     TI* const xs = (TI*)dyn;                        // the element of the row at chunk * E + i
+    const int k = a.weight > 0.f ? a.k : 0;
     float* const tp = (float*)(chunks + share);     // p of the entries, 0 where an entry is left out
-    float* const ts = tp + a.k;                     // the student's logits there (where they are this CTA's)
-    int* const tid = (int*)(ts + a.k);              // their places in the row's chunks, -1 where one is left out
-    __shared__ float sh[6][WARPS];                  // a row of its own for every sum that is joined
-    __shared__ float joined[4][MAX_CLUSTER];
+    float* const ts = tp + k;                       // the student's logits there
+    int* const tid = (int*)(ts + k);                // their places in the CTA's chunks, -1: left out, or not this CTA's
+    int* const raw_ids = tid + k;                   // the entries as they arrive, for this row and the next
+    float* const raw_t = (float*)(raw_ids + 2 * k);
+    unsigned* const seen = (unsigned*)(raw_t + 2 * k);       // a bit per place
+    __shared__ float2 sh[5][WARPS];                 // a row of its own for every pair of sums that is joined
+    __shared__ float2 joined[2][MAX_CLUSTER];
+    __shared__ float lost[MAX_CLUSTER];
     const int R = CLUSTER ? ranks : 1, rank = CLUSTER ? (int)(blockIdx.x % R) : 0, V = (int)a.V;
-    const long row = blockIdx.x / R;
-    const TI* const x = (const TI*)a.logits + row * a.logits_stride;
-    TO* const g = a.grad ? (TO*)a.grad + row * a.grad_stride : nullptr;
-    const int phase = (int)((uintptr_t)x / sizeof(TI) % E);                 // place of the row's first element
-    const int first = rank * share, n = max(0, min(share, (V + phase + E - 1) / E - first));        // this CTA's chunks
-    const int label = a.labels ? a.labels[row] : 0;
-    if (label < 0 || label >= V) {                  // the row does not count
-        if (rank == 0 && threadIdx.x == 0) a.loss[row] = 0.f;
-        const int lo = max(0, first * E - phase), hi = min(V, (first + n) * E - phase);
-        if (g) for (int v = lo + threadIdx.x; v < hi; v += THREADS) st(g + v, 0.f);
-        return;
-    }
-    // over the cluster, the same value everywhere
-    auto join = [&](float v, auto f, int slot) {
-        v = reduce_warp(v, f);
+    const long step = gridDim.x / R;
+    if (CLUSTER) cluster_arrive();                  // waited for before anyone writes to another CTA's shared memory
+    bool started = !CLUSTER;
+    const int first = rank * share;                 // this CTA's chunks of every row
+
+    // of a row: its logits, the place of its first element in its first chunk, how many of the chunks are this CTA's
+    struct Row { const TI* x; int phase, n; };
+    auto row_of = [&](long r) {
+        Row q;
+        q.x = (const TI*)a.logits + r * a.logits_stride;
+        q.phase = (int)((uintptr_t)q.x / sizeof(TI) % E);
+        q.n = max(0, min(share, (V + q.phase + E - 1) / E - first));
+        return q;
+    };
+    const auto inside = [&](const Row& q, int c) { return (first + c) * E >= q.phase && (first + c + 1) * E <= V + q.phase; };      // the whole chunk lies in the row
+    auto fetch = [&](const Row& q, int c) {
+        const long v = (long)(first + c) * E - q.phase;
+        if (inside(q, c)) copy16(chunks + c, q.x + v);
+        else
+            for (int i = 0; i < E; ++i) {
+                if (v + i >= 0 && v + i < V) xs[c * E + i] = q.x[v + i];
+                else st(xs + c * E + i, -INFINITY);
+            }
+    };
+    auto fetch_entries = [&](long r, int buf) {
+        for (int j = threadIdx.x; j < k; j += THREADS) { copy4(raw_ids + buf * k + j, a.ids + r * k + j); copy4(raw_t + buf * k + j, a.teacher + r * k + j); }
+    };
+    // over the cluster, the same values everywhere
+    auto join = [&](float2 v, auto f, int slot) {
+        v.x = reduce_warp(v.x, f); v.y = reduce_warp(v.y, f);
         if ((threadIdx.x & 31) == 0) sh[slot][threadIdx.x >> 5] = v;
         __syncthreads();
         v = sh[slot][0];
 #pragma unroll
-        for (int i = 1; i < WARPS; ++i) v = f(v, sh[slot][i]);
+        for (int i = 1; i < WARPS; ++i) { v.x = f(v.x, sh[slot][i].x); v.y = f(v.y, sh[slot][i].y); }
         if (CLUSTER) {
             cg::cluster_group cl = cg::this_cluster();
+            if (!started) { cluster_wait(); started = true; }
             if (threadIdx.x < R) *cl.map_shared_rank(&joined[slot][rank], threadIdx.x) = v;
-            cl.sync();
+            cluster_arrive();
+            cluster_wait();
             v = joined[slot][0];
-            for (int r = 1; r < R; ++r) v = f(v, joined[slot][r]);
+            for (int r = 1; r < R; ++r) { v.x = f(v.x, joined[slot][r].x); v.y = f(v.y, joined[slot][r].y); }
         }
         return v;
     };
-    const auto inside = [&](int c) { return (first + c) * E >= phase && (first + c + 1) * E <= V + phase; };      // the whole chunk lies in the row
-    const int part = (n + PARTS - 1) / PARTS;
-#pragma unroll
-    for (int q = 0; q < PARTS; ++q) {
-        for (int c = q * part + threadIdx.x; c < min(n, (q + 1) * part); c += THREADS) {
-            const long v = (long)(first + c) * E - phase;
-            if (inside(c)) copy16(chunks + c, x + v);
-            else
-                for (int i = 0; i < E; ++i) {
-                    if (v + i >= 0 && v + i < V) xs[c * E + i] = x[v + i];
-                    else st(xs + c * E + i, -INFINITY);
-                }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    if (CLUSTER) cg::this_cluster().sync();         // every CTA is there before anyone writes to its shared memory
-    const float itau = 1.f / a.tau;
-    const Exps<SQ, HARD> exps{itau * LOG2E};
-    // the teacher, while the row arrives
-    const int k = a.weight > 0.f ? a.k : 0;
-    float tm = -INFINITY;
-    for (int j = threadIdx.x; j < k; j += THREADS) {
-        const int id = a.ids[row * a.k + j];
-        const bool in = id >= 0 && id < V;
-        tid[j] = in ? id + phase : -1;
-        tp[j] = in ? a.teacher[row * a.k + j] : -INFINITY;
-        tm = fmaxf(tm, tp[j]);
-    }
     auto join_cta = [&](float v, auto f, int slot) {
         v = reduce_warp(v, f);
-        if ((threadIdx.x & 31) == 0) sh[slot][threadIdx.x >> 5] = v;
+        if ((threadIdx.x & 31) == 0) sh[slot][threadIdx.x >> 5].x = v;
         __syncthreads();
-        v = sh[slot][0];
+        v = sh[slot][0].x;
 #pragma unroll
-        for (int i = 1; i < WARPS; ++i) v = f(v, sh[slot][i]);
+        for (int i = 1; i < WARPS; ++i) v = f(v, sh[slot][i].x);
         return v;
     };
-    bool taught = false;
-    float logtz = 0.f, inv = 0.f;
-    if (k) {
-        tm = join_cta(tm, Max(), 4);
-        taught = tm != -INFINITY;                   // without an entry that has any weight the term is nothing
-        float tz = 0.f;
-        for (int j = threadIdx.x; j < k; j += THREADS) tz += expf((tp[j] - tm) * itau);
-        tz = join_cta(tz, Add(), 5);
-        logtz = logf(tz); inv = 1.f / tz;
-    }
-    // the row's maximum
-    Terms t{-INFINITY, 0.f, HARD ? 1.f - a.weight : 0.f, 0.f, 0.f, a.scale};
-    auto scan = [&](int q) {
-        for (int c = q * part + threadIdx.x; c < min(n, (q + 1) * part); c += THREADS) {
-            float v[E];
-            unpack(chunks[c], v);
-#pragma unroll
-            for (int i = 0; i < E; ++i) t.m = fmaxf(t.m, v[i]);
-        }
-    };
-    copies_arrived<3>(); scan(0);
-    copies_arrived<2>(); scan(1);
-    copies_arrived<1>(); scan(2);
-    copies_arrived<0>(); scan(3);
-    t.m = join(t.m, Max(), 0);
-    // its sums
-    float zt = 0.f, z1 = 0.f;
+    const float itau = 1.f / a.tau;
+    const Exps<SQ, HARD> exps{itau * LOG2E};
+    long row = blockIdx.x / R;
+    Row q = row_of(row);
+    for (int c = threadIdx.x; c < q.n; c += THREADS) fetch(q, c);
+    fetch_entries(row, 0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (k) for (int i = threadIdx.x; i < (share * E + 31) / 32; i += THREADS) seen[i] = 0;       // (a barrier follows before it is used)
+    int label = a.labels ? a.labels[row] : 0;
+    for (int buf = 0; row < a.M; row += step, buf ^= 1) {
+        const bool more = row + step < a.M;
+        const Row next = more ? row_of(row + step) : Row{nullptr, 0, 0};
+        const int next_label = more && a.labels ? a.labels[row + step] : 0;
+        const bool counts = label >= 0 && label < V;
+        TO* const g = a.grad ? (TO*)a.grad + row * a.grad_stride : nullptr;
+        const int n = q.n;
+        Terms t{-INFINITY, 0.f, HARD ? 1.f - a.weight : 0.f, 0.f, 0.f, a.scale};
+        bool taught = false;
+        float loss = 0.f;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const int hit = HARD && counts ? label + q.phase - first * E : -1;       // the label's place
+        const bool own = hit >= 0 && hit < n * E;
+        float hit_s = 0.f;
+        if (counts) {
+            // the row's maximum, the teacher's
+            float tm = -INFINITY;
+            for (int j = threadIdx.x; j < k; j += THREADS) {
+                const int id = raw_ids[buf * k + j], at = id + q.phase - first * E;
+                const bool in = id >= 0 && id < V;
+                tid[j] = in && at >= 0 && at < n * E ? at : -1;
+                tp[j] = in ? raw_t[buf * k + j] : -INFINITY;
+                tm = fmaxf(tm, tp[j]);
+            }
+            Top top;
+            for (int c = threadIdx.x; c < n; c += THREADS) top.add(chunks[c], TI());
+            if (k) tm = join_cta(tm, Max(), 2);
+            taught = tm != -INFINITY;               // without an entry that has any weight the term is nothing
+            t.m = join(make_float2(top.value(), -INFINITY), Max(), 0).x;         // (its barrier: the whole row is there for everyone)
+            const float2 minus = make_float2(-t.m, -t.m);
+            // sums
+            float tz = 0.f;
+            if (taught) for (int j = threadIdx.x; j < k; j += THREADS) tz += expf((tp[j] - tm) * itau);
+            float2 sums = make_float2(0.f, 0.f);
 #pragma unroll 2
-    for (int c = threadIdx.x; c < n; c += THREADS) {
-        float v[E], st_ = 0.f, s1 = 0.f;
-        unpack(chunks[c], v);
+            for (int c = threadIdx.x; c < n; c += THREADS) {
+                float2 v[E / 2], st_ = make_float2(0.f, 0.f), s1 = st_;
+                unpack(chunks[c], v);
 #pragma unroll
-        for (int i = 0; i < E; ++i) { float et, e1; exps(v[i] - t.m, et, e1); st_ += et; s1 += e1; }
-        zt += st_; z1 += s1;
-    }
-    zt = join(zt, Add(), 1);
-    if (HARD) z1 = join(z1, Add(), 2);
-    float loss = 0.f;
-    if (taught) {
-        const float logz = logf(zt);
-        for (int j = threadIdx.x; j < k; j += THREADS) {
-            const float d = (tp[j] - tm) * itau, p = expf(d) * inv;
-            tp[j] = p;
-            const int at = tid[j] - first * E;
-            if (tid[j] < 0 || at < 0 || at >= n * E) { tid[j] = -1; continue; }     // not this CTA's
-            tid[j] = at;
-            ts[j] = ld(xs + at);
-            if (p != 0.f) loss += p * ((d - logtz) - ((ts[j] - t.m) * itau - logz));
+                for (int i = 0; i < E / 2; ++i) { float2 et, e1; exps(__fadd2_rn(v[i], minus), et, e1); st_ = __fadd2_rn(st_, et); s1 = __fadd2_rn(s1, e1); }
+                sums = __fadd2_rn(sums, make_float2(st_.x + st_.y, s1.x + s1.y));
+            }
+            if (taught) tz = join_cta(tz, Add(), 3);
+            sums = join(sums, Add(), 1);
+            const float zt = sums.x, z1 = sums.y;
+            if (taught) {
+                const float logz = logf(zt), logtz = logf(tz), inv = 1.f / tz;
+                for (int j = threadIdx.x; j < k; j += THREADS) {
+                    const float d = (tp[j] - tm) * itau, p = expf(d) * inv;
+                    tp[j] = p;
+                    if (tid[j] < 0) continue;
+                    ts[j] = ld(xs + tid[j]);
+                    if (p != 0.f) loss += p * ((d - logtz) - ((ts[j] - t.m) * itau - logz));
+                }
+                loss *= a.weight * a.tau * a.tau;
+            }
+            if (own) hit_s = ld(xs + hit);
+            if (HARD && own && threadIdx.x == 0) loss += t.c1 * (logf(z1) - (hit_s - t.m));
+            loss = join_cta(loss, Add(), 4);        // (its barrier: what is needed of the row beside its chunks has been read)
+            if (CLUSTER) {                          // waited for at the row's end
+                if (threadIdx.x == 0) *cg::this_cluster().map_shared_rank(&lost[rank], 0) = loss;
+                cluster_arrive();
+            }
+            t.ct = taught ? a.weight * a.tau : 0.f; t.it = 1.f / zt; t.i1 = HARD ? 1.f / z1 : 0.f;
         }
-        loss *= a.weight * a.tau * a.tau;
-    }
-    const int hit = HARD ? label + phase - first * E : -1;                   // the label's place
-    const bool own = hit >= 0 && hit < n * E;
-    if (HARD && own && threadIdx.x == 0) loss += t.c1 * (logf(z1) - (ld(xs + hit) - t.m));
-    loss = join(loss, Add(), 3);
-    if (rank == 0 && threadIdx.x == 0) a.loss[row] = loss;
-    if (!g) return;
-    t.ct = taught ? a.weight * a.tau : 0.f; t.it = 1.f / zt; t.i1 = HARD ? 1.f / z1 : 0.f;
-    // the gradient without label and entries
-    {
-        const float A = t.scale * t.ct * t.it, B = t.scale * t.c1 * t.i1;
-        const bool vec = (uintptr_t)(g - phase) % (E * sizeof(TO)) == 0;     // the chunks of g start where those of x do
+        if (!CLUSTER && threadIdx.x == 0) a.loss[row] = loss;
+        // the gradient without label and entries; the next row takes the place of this one
+        {
+            const float A = t.scale * t.ct * t.it, B = t.scale * t.c1 * t.i1;
+            const float2 minus = make_float2(-t.m, -t.m);
+            const bool vec = (uintptr_t)(g - q.phase) % (E * sizeof(TO)) == 0;   // the chunks of g start where those of x do
 #pragma unroll 2
-        for (int c = threadIdx.x; c < n; c += THREADS) {
-            float v[E];
-            unpack(chunks[c], v);
+            for (int c = threadIdx.x; c < max(n, next.n); c += THREADS) {
+                uint4 r{};
+                if (c < n) r = chunks[c];
+                if (c < next.n) fetch(next, c);
+                if (!g || c >= n) continue;
+                float2 v[E / 2];
+                unpack(r, v);
 #pragma unroll
-            for (int i = 0; i < E; ++i) { float et, e1; exps(v[i] - t.m, et, e1); v[i] = HARD ? fmaf(A, et, B * e1) : A * et; }
-            const long at = (long)(first + c) * E - phase;
-            if (vec && inside(c)) put(g + at, v);
-            else
+                for (int i = 0; i < E / 2; ++i) {
+                    float2 et, e1;
+                    exps(__fadd2_rn(v[i], minus), et, e1);
+                    v[i] = HARD ? __ffma2_rn(make_float2(A, A), et, __fmul2_rn(make_float2(B, B), e1)) : __fmul2_rn(make_float2(A, A), et);
+                    if (!counts) v[i] = make_float2(0.f, 0.f);
+                }
+                const long at = (long)(first + c) * E - q.phase;
+                if (vec && inside(q, c)) put(g + at, v);
+                else
 #pragma unroll
-                for (int i = 0; i < E; ++i) if (at + i >= 0 && at + i < V) st(g + at + i, v[i]);
+                    for (int i = 0; i < E; ++i) if (at + i >= 0 && at + i < V) st(g + at + i, i & 1 ? v[i / 2].y : v[i / 2].x);
+            }
         }
+        if (more) fetch_entries(row + step, buf ^ 1);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // those, over it
+        if (g && counts) {
+            const long base = (long)first * E - q.phase;
+            auto fix = [&](int at, float s, float p) { float et, e1; exps(s - t.m, et, e1); st(g + base + at, t.at(et, e1, p, HARD && at == hit)); };
+            __syncthreads();
+            if (own && threadIdx.x == 0) fix(hit, hit_s, 0.f);
+            if (taught) {
+                int twice = 0;                      // does an id occur twice?
+                for (int j = threadIdx.x; j < k; j += THREADS)
+                    if (tid[j] >= 0) { const unsigned bit = 1u << (tid[j] & 31); twice |= (atomicOr(seen + (tid[j] >> 5), bit) & bit) != 0; }
+                if (!__syncthreads_or(twice)) {
+                    for (int j = threadIdx.x; j < k; j += THREADS) if (tid[j] >= 0) fix(tid[j], ts[j], tp[j]);
+                } else {
+                    for (int j = threadIdx.x; j < k; j += THREADS) {
+                        if (tid[j] < 0) continue;
+                        float p = 0.f;              // an id that occurs more than once is its first entry's
+                        bool one = true;
+                        for (int i = 0; i < k; ++i) if (tid[i] == tid[j]) { if (i < j) one = false; p += tp[i]; }
+                        if (one) fix(tid[j], ts[j], p);
+                    }
+                    __syncthreads();                // nobody reads the others' entries any more
+                }
+                for (int j = threadIdx.x; j < k; j += THREADS) if (tid[j] >= 0) seen[tid[j] >> 5] = 0;
+            }
+        }
+        if (CLUSTER) {
+            if (counts) cluster_wait();
+            if (rank == 0 && threadIdx.x == 0) {
+                if (counts) for (int r = 1; r < R; ++r) loss += lost[r];
+                a.loss[row] = loss;
+            }
+        }
+        q = next;
+        label = next_label;
     }
-    // those, over it
-    const long base = (long)first * E - phase;
-    auto fix = [&](int at, float s, float p) { float et, e1; exps(s - t.m, et, e1); st(g + base + at, t.at(et, e1, p, HARD && at == hit)); };
-    const float hit_s = own ? ld(xs + hit) : 0.f;
-    __syncthreads();
-    if (own && threadIdx.x == 0) fix(hit, hit_s, 0.f);
-    if (!taught) return;
-    // Does an id occur twice?  Every entry writes its number to its place of the row, which is not needed any more, and looks which one stayed.
-    for (int j = threadIdx.x; j < k; j += THREADS) if (tid[j] >= 0) ((unsigned short*)dyn)[tid[j] * (sizeof(TI) / 2)] = (unsigned short)j;
-    __syncthreads();
-    int twice = 0;
-    for (int j = threadIdx.x; j < k; j += THREADS) if (tid[j] >= 0) twice |= ((unsigned short*)dyn)[tid[j] * (sizeof(TI) / 2)] != j;
-    if (!__syncthreads_or(twice)) {
-        for (int j = threadIdx.x; j < k; j += THREADS) if (tid[j] >= 0) fix(tid[j], ts[j], tp[j]);
-        return;
-    }
-    for (int j = threadIdx.x; j < k; j += THREADS) {
-        if (tid[j] < 0) continue;
-        float p = 0.f;                              // an id that occurs more than once is its first entry's
-        bool first_ = true;
-        for (int i = 0; i < k; ++i) if (tid[i] == tid[j]) { if (i < j) first_ = false; p += tp[i]; }
-        if (first_) fix(tid[j], ts[j], p);
-    }
+    if (CLUSTER && !started) cluster_wait();
 }
+
+// How many clusters of R CTAs the device holds at once (asked for once per size: clusters need their SMs in one part of the device, so it is not SMs x CTAs / R).
+struct Resident {
+    std::atomic<uint64_t> last{0};                  // device, size and R of the last question, and its answer
+    int ask(const void* kernel, int R, int threads, int smem) {
+        int dev = 0;
+        cudaGetDevice(&dev);
+        const uint64_t key = (uint64_t)(dev + 1) << 52 | (uint64_t)R << 44 | (uint64_t)smem << 16, known = last.load(std::memory_order_relaxed);
+        if ((known & ~0xffffull) == key) return (int)(known & 0xffff);
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = R; at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.gridDim = R * 148; cfg.blockDim = threads; cfg.dynamicSmemBytes = smem; cfg.attrs = at; cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+        n = n < 1 ? 1 : n > 0xffff ? 0xffff : n;
+        last.store(key | (uint64_t)n, std::memory_order_relaxed);
+        return n;
+    }
+};
 
 template <typename TI, typename TO, int SQ, bool HARD>
 cudaError_t launch(const DistillArgs& a, cudaStream_t s) {
     if (a.V <= WARP_VOCAB && a.k <= WARP_TOP)
         return klaunch(distill_warp_k<TI, TO, SQ, HARD>, (unsigned)((a.M + WARPS - 1) / WARPS), THREADS, 0, s, a);
-    // A CTA's share of a row: at most 64 KB, so that three fit on an SM and one copies while others compute; smaller where there are too few rows for the
-    // SMs, down to 16 KB
+    // A CTA's share of a row: up to 64 KB with 256 threads, three to an SM, else up to 100 KB with 512 threads, two to an SM: one copies while others compute.  Smaller
+    // where there are too few rows for the SMs, down to 16 KB.
     constexpr int E = Chunk<TI>::E;
     const long chunks = (a.V + E - 1) / E + 1;      // with one more for a row that starts inside a chunk
     int R = 1;
-    while (R < MAX_CLUSTER && chunks > 4096l * R) R *= 2;
+    while (R < MAX_CLUSTER && chunks > 6400l * R) R *= 2;
     while (R < MAX_CLUSTER && a.M * R < 148 && chunks > 1024l * R) R *= 2;
     const int share = (int)((chunks + R - 1) / R);
-    const size_t smem = (size_t)share * 16 + (size_t)a.k * 12;
-    constexpr int most = (int)((DISTILL_MAX_VOCAB / E + 1 + MAX_CLUSTER - 1) / MAX_CLUSTER) * 16 + DISTILL_MAX_TOP * 12;
-    static_assert(most <= 200 * 1024 && most >= 4096 * 16 + DISTILL_MAX_TOP * 12, "shares fit");
-    if (R > 1) {
-        static OncePerDevice once;
-        const cudaError_t e = allow_smem(once, (const void*)distill_row_k<TI, TO, SQ, HARD, true>, most);
+    auto bytes = [](int share, int k) { return share * 16 + k * 28 + (share * E + 31) / 32 * 4; };
+    const int smem = bytes(share, a.weight > 0.f ? a.k : 0), most = bytes(std::max(6400, (int)((DISTILL_MAX_VOCAB / E + 1 + MAX_CLUSTER - 1) / MAX_CLUSTER)), DISTILL_MAX_TOP);
+    auto go = [&](auto kernel, OncePerDevice& once, Resident& resident, int threads) {
+        const cudaError_t e = allow_smem(once, (const void*)kernel, most);
         if (e != cudaSuccess) return e;
-        return klaunch_cluster(distill_row_k<TI, TO, SQ, HARD, true>, (unsigned)(a.M * R), THREADS, smem, s, R, a, R, share);
-    }
-    static OncePerDevice once;
-    const cudaError_t e = allow_smem(once, (const void*)distill_row_k<TI, TO, SQ, HARD, false>, most);
-    if (e != cudaSuccess) return e;
-    return klaunch(distill_row_k<TI, TO, SQ, HARD, false>, (unsigned)a.M, THREADS, smem, s, a, 1, share);
+        const long rows = std::min<long>(a.M, R > 1 ? resident.ask((const void*)kernel, R, threads, smem) : 148 * (threads == 256 ? 3 : 2));      // at once
+        return klaunch_cluster(kernel, (unsigned)(rows * R), threads, (size_t)smem, s, R > 1 ? R : 0, a, R, share);
+    };
+    static OncePerDevice once[4];
+    static Resident resident[4];
+    if (share > 4096) return R > 1 ? go(distill_row_k<TI, TO, SQ, HARD, true, 512>, once[0], resident[0], 512) : go(distill_row_k<TI, TO, SQ, HARD, false, 512>, once[1], resident[1], 512);
+    return R > 1 ? go(distill_row_k<TI, TO, SQ, HARD, true, 256>, once[2], resident[2], 256) : go(distill_row_k<TI, TO, SQ, HARD, false, 256>, once[3], resident[3], 256);
 }
 template <typename TI, typename TO>
 cudaError_t pick(const DistillArgs& a, cudaStream_t s) {
     if (!(a.weight < 1.f)) return launch<TI, TO, -1, false>(a, s);
     return a.tau == 1.f ? launch<TI, TO, 0, true>(a, s) : a.tau == 2.f ? launch<TI, TO, 1, true>(a, s) : a.tau == 4.f ? launch<TI, TO, 2, true>(a, s)
-           : a.tau == 8.f ? launch<TI, TO, 3, true>(a, s) : launch<TI, TO, -1, true>(a, s);
+           : launch<TI, TO, -1, true>(a, s);
 }
 
 }  // namespace
