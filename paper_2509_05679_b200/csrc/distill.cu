@@ -205,8 +205,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k
     int* const raw_ids = tid + k;                   // the entries as they arrive, for this row and the next
     float* const raw_t = (float*)(raw_ids + 2 * k);
     unsigned* const seen = (unsigned*)(raw_t + 2 * k);       // a bit per place
-    __shared__ float2 sh[5][WARPS];                 // a row of its own for every pair of sums that is joined
-    __shared__ float2 joined[2][MAX_CLUSTER];
+    __shared__ float sh[3][3][WARPS];               // of the warps, for every join
+    __shared__ float joined[2][3][MAX_CLUSTER];     // of the CTAs
     __shared__ float lost[MAX_CLUSTER];
     const int R = CLUSTER ? ranks : 1, rank = CLUSTER ? (int)(blockIdx.x % R) : 0, V = (int)a.V;
     const long step = gridDim.x / R;
@@ -214,61 +214,71 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k
     bool started = !CLUSTER;
     const int first = rank * share;                 // this CTA's chunks of every row
 
-    // of a row: its logits, the place of its first element in its first chunk, how many of the chunks are this CTA's
-    struct Row { const TI* x; int phase, n; };
+    // of a row: its logits, the place of its first element in its first chunk, how many of the chunks are this CTA's, and which of these lie in the row altogether
+    struct Row { const TI* x; int phase, n, lo, whole; };
     auto row_of = [&](long r) {
         Row q;
         q.x = (const TI*)a.logits + r * a.logits_stride;
         q.phase = (int)((uintptr_t)q.x / sizeof(TI) % E);
         q.n = max(0, min(share, (V + q.phase + E - 1) / E - first));
+        q.lo = first == 0 && q.phase ? 1 : 0;
+        q.whole = max(0, min(q.n, (V + q.phase) / E - first) - q.lo);
         return q;
     };
-    const auto inside = [&](const Row& q, int c) { return (first + c) * E >= q.phase && (first + c + 1) * E <= V + q.phase; };      // the whole chunk lies in the row
-    auto fetch = [&](const Row& q, int c) {
-        const long v = (long)(first + c) * E - q.phase;
-        if (inside(q, c)) copy16(chunks + c, q.x + v);
-        else
+    const auto inside = [&](const Row& q, int c) { return (unsigned)(c - q.lo) < (unsigned)q.whole; };
+    auto chunk_of = [&](const Row& q, int c) { return (const char*)(q.x + ((long)first * E - q.phase)) + (long)c * 16; };
+    auto fetch = [&](const Row& q, int c, const char* from) {
+        if (inside(q, c)) copy16(chunks + c, from);
+        else {
+            const int v = (first + c) * E - q.phase;
             for (int i = 0; i < E; ++i) {
                 if (v + i >= 0 && v + i < V) xs[c * E + i] = q.x[v + i];
                 else st(xs + c * E + i, -INFINITY);
             }
+        }
     };
     auto fetch_entries = [&](long r, int buf) {
         for (int j = threadIdx.x; j < k; j += THREADS) { copy4(raw_ids + buf * k + j, a.ids + r * k + j); copy4(raw_t + buf * k + j, a.teacher + r * k + j); }
     };
-    // over the cluster, the same values everywhere
-    auto join = [&](float2 v, auto f, int slot) {
-        v.x = reduce_warp(v.x, f); v.y = reduce_warp(v.y, f);
-        if ((threadIdx.x & 31) == 0) sh[slot][threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = sh[slot][0];
+    // NV values each over the CTA, the same in every thread
+    auto join_cta = [&](auto& v, auto f, int slot) {
+        constexpr int NV = sizeof(v) / sizeof(float);
 #pragma unroll
-        for (int i = 1; i < WARPS; ++i) { v.x = f(v.x, sh[slot][i].x); v.y = f(v.y, sh[slot][i].y); }
-        if (CLUSTER) {
-            cg::cluster_group cl = cg::this_cluster();
-            if (!started) { cluster_wait(); started = true; }
-            if (threadIdx.x < R) *cl.map_shared_rank(&joined[slot][rank], threadIdx.x) = v;
-            cluster_arrive();
-            cluster_wait();
-            v = joined[slot][0];
-            for (int r = 1; r < R; ++r) { v.x = f(v.x, joined[slot][r].x); v.y = f(v.y, joined[slot][r].y); }
+        for (int i = 0; i < NV; ++i) {
+            v[i] = reduce_warp(v[i], f);
+            if ((threadIdx.x & 31) == 0) sh[slot][i][threadIdx.x >> 5] = v[i];
         }
-        return v;
-    };
-    auto join_cta = [&](float v, auto f, int slot) {
-        v = reduce_warp(v, f);
-        if ((threadIdx.x & 31) == 0) sh[slot][threadIdx.x >> 5].x = v;
         __syncthreads();
-        v = sh[slot][0].x;
 #pragma unroll
-        for (int i = 1; i < WARPS; ++i) v = f(v, sh[slot][i].x);
-        return v;
+        for (int i = 0; i < NV; ++i) {
+            v[i] = sh[slot][i][threadIdx.x % WARPS];
+#pragma unroll
+            for (int d = WARPS / 2; d; d >>= 1) v[i] = f(v[i], __shfl_xor_sync(~0u, v[i], d));
+        }
+    };
+    // and over the cluster
+    auto join = [&](auto& v, auto f, int slot) {
+        constexpr int NV = sizeof(v) / sizeof(float);
+        join_cta(v, f, slot);
+        if (!CLUSTER) return;
+        cg::cluster_group cl = cg::this_cluster();
+        if (!started) { cluster_wait(); started = true; }
+        if (threadIdx.x < R)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) *cl.map_shared_rank(&joined[slot][i][rank], threadIdx.x) = v[i];
+        cluster_arrive();
+        cluster_wait();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] = joined[slot][i][0];
+            for (int r = 1; r < R; ++r) v[i] = f(v[i], joined[slot][i][r]);
+        }
     };
     const float itau = 1.f / a.tau;
     const Exps<SQ, HARD> exps{itau * LOG2E};
     long row = blockIdx.x / R;
     Row q = row_of(row);
-    for (int c = threadIdx.x; c < q.n; c += THREADS) fetch(q, c);
+    for (int c = threadIdx.x; c < q.n; c += THREADS) fetch(q, c, chunk_of(q, c));
     fetch_entries(row, 0);
     asm volatile("cp.async.commit_group;" ::: "memory");
     if (k) for (int i = threadIdx.x; i < (share * E + 31) / 32; i += THREADS) seen[i] = 0;       // (a barrier follows before it is used)
@@ -289,35 +299,38 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k
         float hit_s = 0.f;
         if (counts) {
             // the row's maximum, the teacher's
-            float tm = -INFINITY;
+            float most[2] = {-INFINITY, -INFINITY};
             for (int j = threadIdx.x; j < k; j += THREADS) {
                 const int id = raw_ids[buf * k + j], at = id + q.phase - first * E;
                 const bool in = id >= 0 && id < V;
                 tid[j] = in && at >= 0 && at < n * E ? at : -1;
                 tp[j] = in ? raw_t[buf * k + j] : -INFINITY;
-                tm = fmaxf(tm, tp[j]);
+                most[1] = fmaxf(most[1], tp[j]);
             }
             Top top;
+#pragma unroll 4
             for (int c = threadIdx.x; c < n; c += THREADS) top.add(chunks[c], TI());
-            if (k) tm = join_cta(tm, Max(), 2);
+            most[0] = top.value();
+            join(most, Max(), 0);                   // (its barrier: the whole row is there for everyone)
+            t.m = most[0];
+            const float tm = most[1];
             taught = tm != -INFINITY;               // without an entry that has any weight the term is nothing
-            t.m = join(make_float2(top.value(), -INFINITY), Max(), 0).x;         // (its barrier: the whole row is there for everyone)
             const float2 minus = make_float2(-t.m, -t.m);
-            // sums
-            float tz = 0.f;
-            if (taught) for (int j = threadIdx.x; j < k; j += THREADS) tz += expf((tp[j] - tm) * itau);
-            float2 sums = make_float2(0.f, 0.f);
+            // sums: at the student's temperatures, of the teacher's (every CTA those entries that are its own)
+            float total[3] = {0.f, 0.f, 0.f};
+            if (taught) for (int j = threadIdx.x; j < k; j += THREADS) if (tid[j] >= 0) total[2] += expf((tp[j] - tm) * itau);
+            float2 sum_t = make_float2(0.f, 0.f), sum_1 = sum_t;
 #pragma unroll 2
             for (int c = threadIdx.x; c < n; c += THREADS) {
                 float2 v[E / 2], st_ = make_float2(0.f, 0.f), s1 = st_;
                 unpack(chunks[c], v);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) { float2 et, e1; exps(__fadd2_rn(v[i], minus), et, e1); st_ = __fadd2_rn(st_, et); s1 = __fadd2_rn(s1, e1); }
-                sums = __fadd2_rn(sums, make_float2(st_.x + st_.y, s1.x + s1.y));
+                sum_t = __fadd2_rn(sum_t, st_); if (HARD) sum_1 = __fadd2_rn(sum_1, s1);
             }
-            if (taught) tz = join_cta(tz, Add(), 3);
-            sums = join(sums, Add(), 1);
-            const float zt = sums.x, z1 = sums.y;
+            total[0] = sum_t.x + sum_t.y; total[1] = sum_1.x + sum_1.y;
+            join(total, Add(), 1);
+            const float zt = total[0], z1 = total[1], tz = total[2];
             if (taught) {
                 const float logz = logf(zt), logtz = logf(tz), inv = 1.f / tz;
                 for (int j = threadIdx.x; j < k; j += THREADS) {
@@ -331,7 +344,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k
             }
             if (own) hit_s = ld(xs + hit);
             if (HARD && own && threadIdx.x == 0) loss += t.c1 * (logf(z1) - (hit_s - t.m));
-            loss = join_cta(loss, Add(), 4);        // (its barrier: what is needed of the row beside its chunks has been read)
+            float part[1] = {loss};
+            join_cta(part, Add(), 2);               // (its barrier: what is needed of the row beside its chunks has been read)
+            loss = part[0];
             if (CLUSTER) {                          // waited for at the row's end
                 if (threadIdx.x == 0) *cg::this_cluster().map_shared_rank(&lost[rank], 0) = loss;
                 cluster_arrive();
@@ -340,31 +355,37 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k
         }
         if (!CLUSTER && threadIdx.x == 0) a.loss[row] = loss;
         // the gradient without label and entries; the next row takes the place of this one
-        {
+        const char* from = more ? chunk_of(next, threadIdx.x) : nullptr;
+        if (g && counts) {
             const float A = t.scale * t.ct * t.it, B = t.scale * t.c1 * t.i1;
-            const float2 minus = make_float2(-t.m, -t.m);
+            const float2 minus = make_float2(-t.m, -t.m), A2 = make_float2(A, A), B2 = make_float2(B, B);
             const bool vec = (uintptr_t)(g - q.phase) % (E * sizeof(TO)) == 0;   // the chunks of g start where those of x do
+            TO* to = g + ((long)first * E - q.phase) + (long)threadIdx.x * E;
 #pragma unroll 2
-            for (int c = threadIdx.x; c < max(n, next.n); c += THREADS) {
+            for (int c = threadIdx.x; c < max(n, next.n); c += THREADS, from += THREADS * 16, to += THREADS * E) {
                 uint4 r{};
                 if (c < n) r = chunks[c];
-                if (c < next.n) fetch(next, c);
-                if (!g || c >= n) continue;
+                if (c < next.n) fetch(next, c, from);
+                if (c >= n) continue;
                 float2 v[E / 2];
                 unpack(r, v);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) {
                     float2 et, e1;
                     exps(__fadd2_rn(v[i], minus), et, e1);
-                    v[i] = HARD ? __ffma2_rn(make_float2(A, A), et, __fmul2_rn(make_float2(B, B), e1)) : __fmul2_rn(make_float2(A, A), et);
-                    if (!counts) v[i] = make_float2(0.f, 0.f);
+                    v[i] = HARD ? __ffma2_rn(A2, et, __fmul2_rn(B2, e1)) : __fmul2_rn(A2, et);
                 }
-                const long at = (long)(first + c) * E - q.phase;
-                if (vec && inside(q, c)) put(g + at, v);
-                else
+                if (vec && inside(q, c)) put(to, v);
+                else {
+                    const int at = (first + c) * E - q.phase;
 #pragma unroll
-                    for (int i = 0; i < E; ++i) if (at + i >= 0 && at + i < V) st(g + at + i, i & 1 ? v[i / 2].y : v[i / 2].x);
+                    for (int i = 0; i < E; ++i) if (at + i >= 0 && at + i < V) st(to + i, i & 1 ? v[i / 2].y : v[i / 2].x);
+                }
             }
+        } else {
+            for (int c = threadIdx.x; c < next.n; c += THREADS, from += THREADS * 16) fetch(next, c, from);
+            if (g)                                  // the row does not count
+                for (int v = max(0, first * E - q.phase) + threadIdx.x; v < min(V, (first + n) * E - q.phase); v += THREADS) st(g + v, 0.f);
         }
         if (more) fetch_entries(row + step, buf ^ 1);
         asm volatile("cp.async.commit_group;" ::: "memory");
