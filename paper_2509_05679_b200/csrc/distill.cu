@@ -24,7 +24,7 @@ __device__ __forceinline__ float ld(const bf16* p) { return __bfloat162float(*p)
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;             // of distill_warp_k
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int MAX_CLUSTER = 8;
 
 // Results below 2^-126 are zero: beside the maximum's exponential, which is 1, that is nothing, and subnormal ones cost three instructions more.
@@ -192,9 +192,9 @@ __device__ __forceinline__ void copy4(void* smem, const void* g) {
 // A row is cut into chunks of 16 aligned bytes, the first and the last one partly outside the row (there: -infinity).  A thread copies, and in every pass
 // handles, the chunks threadIdx.x, + THREADS, ... of its CTA's share, so that it can have the next row's chunk copied to where it has just read this one's for the last
 // time: a CTA (or cluster) goes through the rows row0, + step, ... with the next row on its way while the gradient of this one is written.
-template <typename TI, typename TO, int SQ, bool HARD, bool CLUSTER, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k(DistillArgs a, int ranks, int share) {
-    constexpr int WARPS = THREADS / 32, E = Chunk<TI>::E;
+template <typename TI, typename TO, int SQ, bool HARD, bool CLUSTER>
+__global__ void __launch_bounds__(THREADS, 3) distill_row_k(DistillArgs a, int ranks, int share) {
+    constexpr int E = Chunk<TI>::E;
     extern __shared__ __align__(16) char dyn[];
     uint4* const chunks = (uint4*)dyn;
     TI* const xs = (TI*)dyn;                        // the element of the row at chunk * E + i
@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 2) distill_row_k
 // How many clusters of R CTAs the device holds at once (asked for once per size: clusters need their SMs in one part of the device, so it is not SMs x CTAs / R).
 struct Resident {
     std::atomic<uint64_t> last{0};                  // device, size and R of the last question, and its answer
-    int ask(const void* kernel, int R, int threads, int smem) {
+    int ask(const void* kernel, int R, int smem) {
         int dev = 0;
         cudaGetDevice(&dev);
         const uint64_t key = (uint64_t)(dev + 1) << 52 | (uint64_t)R << 44 | (uint64_t)smem << 16, known = last.load(std::memory_order_relaxed);
@@ -439,7 +439,7 @@ struct Resident {
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim.x = R; at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-        cfg.gridDim = R * 148; cfg.blockDim = threads; cfg.dynamicSmemBytes = smem; cfg.attrs = at; cfg.numAttrs = 1;
+        cfg.gridDim = R * 148; cfg.blockDim = THREADS; cfg.dynamicSmemBytes = smem; cfg.attrs = at; cfg.numAttrs = 1;
         int n = 0;
         if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
         n = n < 1 ? 1 : n > 0xffff ? 0xffff : n;
@@ -452,8 +452,9 @@ template <typename TI, typename TO, int SQ, bool HARD>
 cudaError_t launch(const DistillArgs& a, cudaStream_t s) {
     if (a.V <= WARP_VOCAB && a.k <= WARP_TOP)
         return klaunch(distill_warp_k<TI, TO, SQ, HARD>, (unsigned)((a.M + WARPS - 1) / WARPS), THREADS, 0, s, a);
-    // A CTA's share of a row: up to 64 KB with 256 threads, three to an SM, else up to 100 KB with 512 threads, two to an SM: one copies while others compute.  Smaller
-    // where there are too few rows for the SMs, down to 16 KB.
+    // A CTA's share of a row: up to 100 KB, so that two fit on an SM (three up to 64 KB) and one copies while others compute; smaller where there are too few rows for
+    // the SMs, down to 16 KB.  1500 rows of 100003 fp32 logits: 271 us in four shares, 327 in eight (more time in the cluster's barriers), 295 in four with 512 threads
+    // a CTA (more time in the joins).
     constexpr int E = Chunk<TI>::E;
     const long chunks = (a.V + E - 1) / E + 1;      // with one more for a row that starts inside a chunk
     int R = 1;
@@ -462,16 +463,19 @@ cudaError_t launch(const DistillArgs& a, cudaStream_t s) {
     const int share = (int)((chunks + R - 1) / R);
     auto bytes = [](int share, int k) { return share * 16 + k * 28 + (share * E + 31) / 32 * 4; };
     const int smem = bytes(share, a.weight > 0.f ? a.k : 0), most = bytes(std::max(6400, (int)((DISTILL_MAX_VOCAB / E + 1 + MAX_CLUSTER - 1) / MAX_CLUSTER)), DISTILL_MAX_TOP);
-    auto go = [&](auto kernel, OncePerDevice& once, Resident& resident, int threads) {
+    if (R > 1) {
+        static OncePerDevice once;
+        static Resident resident;
+        const auto kernel = distill_row_k<TI, TO, SQ, HARD, true>;
         const cudaError_t e = allow_smem(once, (const void*)kernel, most);
         if (e != cudaSuccess) return e;
-        const long rows = std::min<long>(a.M, R > 1 ? resident.ask((const void*)kernel, R, threads, smem) : 148 * (threads == 256 ? 3 : 2));      // at once
-        return klaunch_cluster(kernel, (unsigned)(rows * R), threads, (size_t)smem, s, R > 1 ? R : 0, a, R, share);
-    };
-    static OncePerDevice once[4];
-    static Resident resident[4];
-    if (share > 4096) return R > 1 ? go(distill_row_k<TI, TO, SQ, HARD, true, 512>, once[0], resident[0], 512) : go(distill_row_k<TI, TO, SQ, HARD, false, 512>, once[1], resident[1], 512);
-    return R > 1 ? go(distill_row_k<TI, TO, SQ, HARD, true, 256>, once[2], resident[2], 256) : go(distill_row_k<TI, TO, SQ, HARD, false, 256>, once[3], resident[3], 256);
+        const long rows = std::min<long>(a.M, resident.ask((const void*)kernel, R, smem));       // at once
+        return klaunch_cluster(kernel, (unsigned)(rows * R), THREADS, (size_t)smem, s, R, a, R, share);
+    }
+    static OncePerDevice once;
+    const auto kernel = distill_row_k<TI, TO, SQ, HARD, false>;
+    const cudaError_t e = allow_smem(once, (const void*)kernel, most);
+    return e != cudaSuccess ? e : klaunch(kernel, (unsigned)std::min<long>(a.M, 148 * 3), THREADS, (size_t)smem, s, a, 1, share);
 }
 template <typename TI, typename TO>
 cudaError_t pick(const DistillArgs& a, cudaStream_t s) {
