@@ -6,15 +6,19 @@
 // a launch would otherwise be too small, a cluster its CTAs through distributed shared memory; then every thread runs its steps again from the state in front of
 // them.  The joins are a fixed tree, so equal inputs give equal bits.  Backwards the same with g_t = a_t d_t, the map g -> a (g + dy).
 //
-// Bound: HBM (forward 3 values a step and channel, backward 5).  A CTA walks along its sequence with a ring of tiles that cp.async fills ahead; a thread
-// reads only what it copied itself, so the ring needs no barrier.
+// Bound: HBM (forward 3 values a step and channel, backward 5).  A CTA walks along its sequence with a ring of tiles that tensor copies fill ahead.
 // States are held in 32 bits.  The backward pass computes h again from the states that the forward pass leaves in front of every tile: y rounded to bf16 would
 // put 2^-9 of h into dz, and the states are 2 / (tile's steps) of the bytes of y.
 #include "seqops.h"
 #include "launch.h"
+#include "tc_gemm.h"
 
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 namespace fdg {
 namespace {
@@ -23,15 +27,16 @@ namespace cg = cooperative_groups;
 using bf16 = __nv_bfloat16;
 
 constexpr int THREADS = 256;
-constexpr int STEPS = 4;                // of a thread in a tile
+constexpr int STEPS = 4;                // of a thread in a tile, backwards
+// forward, where there are registers for more, and with fp32 no shared memory
+template <typename T> constexpr int STEPS_FWD = sizeof(T) == 2 ? 8 : 4;
 constexpr int N = 4;                    // channels of a thread
 constexpr int MAX_CLUSTER = 8;      // of slices up to 32 channels; wider ones have no clusters
 
 // CX threads lie along the channels, the others along the steps.
-template <int CX> struct Geo {
-    static constexpr int TG = THREADS / CX, CH = CX * N, TILE = TG * STEPS;
+template <int CX, int S> struct Geo {
+    static constexpr int TG = THREADS / CX, CH = CX * N, TILE = TG * S;
     static constexpr int TEAM = CX < 32 ? 32 : CX, TEAMS = THREADS / TEAM;      // a team joins its threads by shuffles (or is one step group)
-    static constexpr int RANKS = CX > 8 ? 1 : MAX_CLUSTER;
 };
 
 // Values go in pairs through the packed fp32 instructions: the kernels issue too much, not too little, to keep up with HBM.
@@ -67,30 +72,98 @@ __device__ __forceinline__ void pack(const Four& x, uint2& r) {
     const __nv_bfloat162 lo = __float22bfloat162_rn(x.p[0]), hi = __float22bfloat162_rn(x.p[1]);
     r = make_uint2(*(const unsigned*)&lo, *(const unsigned*)&hi);
 }
-// a step that changes nothing: gate open (+infinity), value and dy zero
-__device__ __forceinline__ void idle(float4* z, float4* x) { *z = make_float4(INFINITY, INFINITY, INFINITY, INFINITY); *x = make_float4(0.f, 0.f, 0.f, 0.f); }
-__device__ __forceinline__ void idle(uint2* z, uint2* x) { *z = make_uint2(0x7f807f80u, 0x7f807f80u); *x = make_uint2(0u, 0u); }
 __device__ __forceinline__ float ld(const float* p) { return *p; }
 __device__ __forceinline__ float ld(const bf16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// a step that changes nothing: gate open (+infinity), value and dy zero
+__device__ __forceinline__ void idle(Four& z, Four& x) { z = {both(INFINITY), both(INFINITY)}; x = {both(0.f), both(0.f)}; }
+
+// ---- tiles on their way through shared memory
 template <int BYTES> __device__ __forceinline__ void copy_async(void* smem, const void* g) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((unsigned)__cvta_generic_to_shared(smem)), "l"(g), "n"(BYTES) : "memory");
 }
-__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-
-// ACC: elements that a copy moves at once, as the addresses allow: 4, 2 (bf16), 1.  A single bf16 is too little for cp.async.
-template <typename T, int ACC> __device__ __forceinline__ void fetch(void* slot, const T* g, int left) {
-    if constexpr (ACC * sizeof(T) >= 4) {
-#pragma unroll
-        for (int j = 0; j < N; j += ACC) if (ACC == N || j < left) copy_async<ACC * sizeof(T)>((T*)slot + j, g + j);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (j < left) ((T*)slot)[j] = g[j];
-    }
+__device__ __forceinline__ unsigned smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool try_wait(const uint64_t* bar, unsigned parity) {
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok;
 }
+constexpr long long WAIT_CYCLES = 4000000000ll;      // about 2 s
+// The maps of gate, value and dy; used by the kernels whose rows lie on 16 bytes.
+struct Maps { tc::TensorMap t[3]; };
+
+// ACC: elements that can be moved at once, as the addresses allow.  16 bytes: tensor copies (TMA), one thread for the CTA; their arrival is signalled on a barrier per
+// stage.  4 bytes: cp.async, less: plain loads; there every thread copies what it reads itself, and waits for its own copies.
+template <typename T, int ACC, int CX, int S, int TENSORS> struct Ring {
+    using V = typename Raw<T>::V;
+    using G = Geo<CX, S>;
+    static constexpr bool TMA = ACC * sizeof(T) == 16;
+    static constexpr int STAGES = sizeof(T) == 2 ? 3 : 2, ROW = G::CH * (int)sizeof(T), TENSOR = G::TILE * ROW, STAGE = TENSORS * TENSOR, BYTES = STAGES * STAGE;
+    static constexpr int BOX = G::TILE < 256 ? G::TILE : 256;      // rows of a tensor copy
+    char* base;                                      // on 128 bytes
+    uint64_t* full;                                  // [STAGES]
+    bool gave_up = false;
+    __device__ __forceinline__ char* mine(int stage, int tensor, int i) const {
+        return base + stage * STAGE + tensor * TENSOR + (threadIdx.x / CX * S + i) * ROW + threadIdx.x % CX * (int)sizeof(V);
+    }
+    __device__ __forceinline__ Four get(int stage, int tensor, int i) const { return unpack(*(const V*)mine(stage, tensor, i)); }
+    __device__ __forceinline__ void begin() const {
+        if constexpr (TMA) {
+            if (threadIdx.x == 0) {
+                for (int i = 0; i < STAGES; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(full + i)) : "memory");
+                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            }
+            __syncthreads();
+        }
+    }
+    // rows t .. t + TILE - 1 of sequence b, channels c0 ..; g: this thread's first row and channel of every tensor, `left` of its channels exist, n of its rows count
+    __device__ __forceinline__ void fetch(int stage, const Maps& maps, long c0, int t, long b, const T* const (&g)[TENSORS], const long (&step)[TENSORS], int left, int n) const {
+        if constexpr (TMA) {
+            if (threadIdx.x != 0) return;
+            const unsigned bar = smem_u32(full + stage);
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((unsigned)STAGE) : "memory");
+#pragma unroll
+            for (int q = 0; q < TENSORS; ++q)
+#pragma unroll
+                for (int r = 0; r < G::TILE; r += BOX)
+                    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                                     smem_u32(base + stage * STAGE + q * TENSOR + r * ROW)), "l"(&maps.t[q]), "r"(bar), "r"((int)c0), "r"(t + r), "r"((int)b) : "memory");
+        } else {
+#pragma unroll
+            for (int q = 0; q < TENSORS; ++q)
+#pragma unroll
+                for (int i = 0; i < S; ++i)
+                    if (i < n)
+#pragma unroll
+                        for (int j = 0; j < N; j += ACC)
+                            if (j < left) {
+                                if constexpr (ACC * sizeof(T) >= 4) copy_async<ACC * sizeof(T)>((T*)mine(stage, q, i) + j, g[q] + i * step[q] + j);
+                                else ((T*)mine(stage, q, i))[j] = g[q][i * step[q] + j];
+                            }
+        }
+    }
+    __device__ __forceinline__ void issued() const { if constexpr (!TMA) asm volatile("cp.async.commit_group;" ::: "memory"); }
+    // the round's tile; LEFT: copies issued later that may be under way.  Bounded: a wait that gives up says so, and no other waits.
+    template <int LEFT> __device__ __forceinline__ void arrived(int stage, int round) {
+        if constexpr (TMA) {
+            const unsigned parity = (unsigned)(round / STAGES & 1);
+            if (gave_up || try_wait(full + stage, parity)) return;
+            const long long t0 = clock64();
+            while (!try_wait(full + stage, parity)) if (clock64() - t0 > WAIT_CYCLES) { gave_up = true; return; }
+        } else copies_arrived<LEFT>();
+    }
+    // in front of the end: what a wait that gave up left under way
+    __device__ __forceinline__ void drain(int rounds) const {
+        if constexpr (TMA) {
+            if (!gave_up) return;
+            const long long t0 = clock64();
+            for (int r = max(0, rounds - STAGES); r < rounds; ++r) while (!try_wait(full + r % STAGES, (unsigned)(r / STAGES & 1))) if (clock64() - t0 > WAIT_CYCLES) return;
+        }
+    }
+};
 template <typename T, int ACC> __device__ __forceinline__ void put(T* g, Four x, int left, bool accum) {
     if (accum) {
         if (0 < left) x.p[0].x += ld(g);
@@ -98,7 +171,7 @@ template <typename T, int ACC> __device__ __forceinline__ void put(T* g, Four x,
         if (2 < left) x.p[1].x += ld(g + 2);
         if (3 < left) x.p[1].y += ld(g + 3);
     }
-    if constexpr (ACC == N) {
+    if constexpr (ACC >= N) {
         typename Raw<T>::V r;
         pack(x, r);
         *(typename Raw<T>::V*)g = r;
@@ -112,20 +185,47 @@ template <typename T, int ACC> __device__ __forceinline__ void put(T* g, Four x,
         if (3 < left) st(g + 3, x.p[1].y);
     }
 }
-// steps of t0 .. t0 + STEPS - 1 that lie in front of `end`
-__device__ __forceinline__ int steps_before(int end, int t0) { return min(max(end - t0, 0), STEPS); }
-
-template <typename T, int TENSORS> struct Ring {
-    using V = typename Raw<T>::V;
-    static constexpr int STAGES = sizeof(T) == 2 ? 3 : 2;
-    static constexpr int STAGE = STEPS * TENSORS * THREADS;
-    static constexpr int BYTES = STAGES * STAGE * (int)sizeof(V);
-    V* mine;                                                     // this thread's first slot
-    __device__ V* slot(int stage, int i, int tensor) const { return mine + stage * STAGE + (i * TENSORS + tensor) * THREADS; }
-};
+// steps of t0 .. t0 + S - 1 that lie in front of `end`
+template <int S> __device__ __forceinline__ int steps_before(int end, int t0) { return min(max(end - t0, 0), S); }
 
 __device__ __forceinline__ void store(float* p, const Four& x) { *(float4*)p = make_float4(x.p[0].x, x.p[0].y, x.p[1].x, x.p[1].y); }
 __device__ __forceinline__ Four load(const float* p) { const float4 r = *(const float4*)p; return {make_float2(r.x, r.y), make_float2(r.z, r.w)}; }
+
+// Maps of the CTAs of a cluster, {A, H} per channel, sent into the shared memory of all of them; a barrier counts their bytes.  (A cluster-wide barrier would wait for the
+// outputs under way too, a microsecond a round.)  Two places by the round's parity suffice: whoever has the maps of round k + 1 knows that all have read those of round k.
+template <int CH> struct Joined { float2 at[2][MAX_CLUSTER][CH]; uint64_t bar[2]; };
+template <int CH> struct Peers {
+    Joined<CH>* j;
+    __device__ __forceinline__ void begin() const {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(j->bar + i)) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cg::this_cluster().sync();                               // every CTA is there, and its barriers
+    }
+    // the map of this CTA and thread's channel (threads 0 .. CH - 1)
+    __device__ __forceinline__ void send(int round, int rank, int R, float a, float h) const {
+        if (threadIdx.x == 0)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(j->bar + (round & 1))), "r"((unsigned)(R * CH * sizeof(float2))) : "memory");
+        const unsigned to = smem_u32(&j->at[round & 1][rank][threadIdx.x]), bar = smem_u32(j->bar + (round & 1));
+        for (int r = 0; r < R; ++r) {
+            unsigned t, b;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(t) : "r"(to), "r"(r));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(bar), "r"(r));
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(t), "f"(a), "f"(h), "r"(b) : "memory");
+        }
+    }
+    __device__ __forceinline__ bool arrived(int round) const {
+        const unsigned bar = smem_u32(j->bar + (round & 1)), parity = (unsigned)(round >> 1 & 1);
+        const long long t0 = clock64();
+        for (;;) {
+            unsigned ok;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+            if (ok) return true;
+            if (clock64() - t0 > WAIT_CYCLES) return false;
+        }
+    }
+};
 
 // Joining the maps of a tile.  Up to 32 channels (CX <= 8) a warp holds several step groups: its threads leave their maps in shared memory, and a lane takes one channel
 // and LINKS = 4 of the groups from there; above (a team is one step group) a lane has its own four channels.
@@ -194,16 +294,19 @@ __device__ __forceinline__ void store(float2* p, const Four& A, const Four& H) {
 // One barrier a tile: behind it a warp goes through the maps of the teams in front of it by itself, and the last steps' threads leave the state for the
 // next tile, which the next tile's barrier orders.  What stands there is kept twice, by the round's parity.
 template <typename T, int ACC, int CX, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int ranks, int slices) {
+__global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __grid_constant__ Maps maps, int ranks, int slices) {
     const int R = CLUSTER ? ranks : 1;
-    using G = Geo<CX>;
-    using Rg = Ring<T, 2>;
-    extern __shared__ __align__(16) char dyn[];
-    const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
+    constexpr int S = STEPS_FWD<T>, PARTS = S / STEPS;         // tiles of the backward pass in one of this
+    using G = Geo<CX, S>;
+    using Rg = Ring<T, ACC, CX, S, 2>;
+    extern __shared__ __align__(128) char dyn[];
+    __shared__ uint64_t full[Rg::STAGES];
+    Rg ring{dyn, full};
     __shared__ __align__(16) float2 tot[2][G::TEAMS][G::CH];
     __shared__ __align__(16) float own[2][Lane<CX>::ONE ? THREADS * N : 1];      // a warp's maps, later the states in front of its step groups
     __shared__ __align__(16) float carried[2][G::CH];
-    __shared__ __align__(16) float2 joined[2][G::RANKS][G::CH];
+    __shared__ __align__(16) Joined<CLUSTER ? G::CH : 2> joined;
+    const Peers<CLUSTER ? G::CH : 2> peers{&joined};
     const int rank = CLUSTER ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
@@ -212,24 +315,21 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int ranks
     const int left = (int)min((long)N, p.C - c);                 // channels of this thread that exist
     const int T_ = (int)p.T, len = p.lengths ? min(max(p.lengths[b], 0), T_) : T_;
     const int tiles = (T_ + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = R * G::TILE;
-    int t0 = rank * G::TILE + tg * STEPS, tf = t0;        // this thread's first step: of the round, of the next tile to fetch
-    const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
-    const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
+    const int saves = (T_ + Geo<CX, STEPS>::TILE - 1) / Geo<CX, STEPS>::TILE;
+    int t0 = rank * G::TILE + tg * S, tf = t0;        // this thread's first step: of the round, of the next tile to fetch
+    const T* gf[2] = {(const T*)p.z + b * p.z_b + c + t0 * p.z_t, (const T*)p.v + b * p.v_b + c + t0 * p.v_t};
+    const long step[2] = {p.z_t, p.v_t}, round_step[2] = {stride * p.z_t, stride * p.v_t};
     T* y = (T*)p.y + b * p.y_b + c + t0 * p.y_t;
-    const long z_round = stride * p.z_t, v_round = stride * p.v_t, y_round = stride * p.y_t;
+    const long y_round = stride * p.y_t;
+    const int behind = rounds * stride;                          // the first step that no round looks at
     auto fetch_tile = [&](int stage) {
-        const int n = left > 0 ? steps_before(len, tf) : 0;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-            if (i < n) {
-                fetch<T, ACC>(ring.slot(stage, i, 0), zf + i * p.z_t, left);
-                fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
-            } else idle(ring.slot(stage, i, 0), ring.slot(stage, i, 1));
-        copies_issued();
-        tf += stride; zf += z_round; vf += v_round;
+        if (tf < behind) ring.fetch(stage, maps, c0, tf - tg * S, b, gf, step, left, steps_before<S>(len, tf));
+        ring.issued();
+        tf += stride; gf[0] += round_step[0]; gf[1] += round_step[1];
     };
+    ring.begin();
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
-    if (CLUSTER) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
+    if (CLUSTER) peers.begin();
     const int first = Lane<CX>::first(), mine = (threadIdx.x & ~31) * N;
     Lane<CX> carry;                                              // CLUSTER: the state in front of the round, in every warp
     carry.read(p.state ? p.state + b * p.C : nullptr, c0, p.C);
@@ -237,22 +337,28 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int ranks
     int stage = 0;
     for (int round = 0; round < rounds; ++round) {
         const int now = round & 1;
-        fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
-        copies_arrived<Rg::STAGES - 1>();
+        fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);     // where the tile before was: it has been read
+        ring.template arrived<Rg::STAGES - 1>(stage, round);
         // the map of this thread's steps
-        Four a[STEPS], u[STEPS], A, H;
+        const int n = steps_before<S>(len, t0);
+        Four a[S], u[S], A, H;
+        auto look = [&](auto all) {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const Four z = unpack(*ring.slot(stage, i, 0)), v = unpack(*ring.slot(stage, i, 1));
+            for (int i = 0; i < S; ++i) {
+                Four z = ring.get(stage, 0, i), v = ring.get(stage, 1, i);
+                if (!all.value && i >= n) idle(z, v);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float2 q;
-                gate(z.p[j], a[i].p[j], q);
-                u[i].p[j] = mul(q, v.p[j]);
-                if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u[0].p[j]; }
-                else { H.p[j] = fma(a[i].p[j], H.p[j], u[i].p[j]); A.p[j] = mul(A.p[j], a[i].p[j]); }
+                for (int j = 0; j < 2; ++j) {
+                    float2 q;
+                    gate(z.p[j], a[i].p[j], q);
+                    u[i].p[j] = mul(q, v.p[j]);
+                    if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u[0].p[j]; }
+                    else { H.p[j] = fma(a[i].p[j], H.p[j], u[i].p[j]); A.p[j] = mul(A.p[j], a[i].p[j]); }
+                }
             }
-        }
+        };
+        if (n == S) look(std::true_type()); else look(std::false_type());
+        if (ring.gave_up) u[0] = H = {both(NAN), both(NAN)};
         Chain<CX, true> chain;
         if constexpr (Lane<CX>::ONE) {
             __syncwarp();
@@ -264,39 +370,40 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int ranks
         __syncthreads();
         Lane<CX> in;
         if (CLUSTER) {                                             // the CTA's map goes to every CTA of the cluster
-            cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < G::CH) {
                 float ta = 1.f, th = 0.f;
 #pragma unroll
                 for (int w = 0; w < G::TEAMS; ++w) { const float2 m = tot[now][w][threadIdx.x]; th = fmaf(m.x, th, m.y); ta *= m.x; }
-                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[now][rank][threadIdx.x], r) = make_float2(ta, th);
+                peers.send(round, rank, R, ta, th);
             }
-            cl.sync();
+            if (!ring.gave_up && !peers.arrived(round)) ring.gave_up = true;
             for (int r = 0; r < R; ++r) {
                 if (r == rank) in = carry;
-                carry.through(&joined[now][r][first]);
+                carry.through(&joined.at[now][r][first]);
             }
         } else in.set(&carried[now][first]);
-        if (p.saved && threadIdx.x < G::TEAM && Lane<CX>::writes() && round * R + rank < tiles) in.write(p.saved + ((long)b * tiles + round * R + rank) * p.C, c0, p.C);
         for (int w = 0; w < team; ++w) in.through(&tot[now][w][first]);
+        if (p.saved && team % (G::TEAMS / PARTS) == 0 && Lane<CX>::writes()) {
+            const int at = (round * R + rank) * PARTS + team / (G::TEAMS / PARTS);
+            if (at < saves) in.write(p.saved + ((long)b * saves + at) * p.C, c0, p.C);
+        }
         Four h;
         if constexpr (Lane<CX>::ONE) {
             chain.apply(in.v[0], &own[1][mine]);
             __syncwarp();
             h = load(&own[1][threadIdx.x * N]);
         } else h = {make_float2(in.v[0], in.v[1]), make_float2(in.v[2], in.v[3])};
-        const int n = left > 0 ? steps_before(len, t0) : 0;
-        if (n == STEPS) {
+        if (n == S && left > 0) {
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
+            for (int i = 0; i < S; ++i) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) h.p[j] = fma(a[i].p[j], h.p[j], u[i].p[j]);
                 put<T, ACC>(y + i * p.y_t, h, left, false);
             }
         } else {
-            const int out = left > 0 ? steps_before(T_, t0) : 0;
+            const int out = left > 0 ? steps_before<S>(T_, t0) : 0;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
+            for (int i = 0; i < S; ++i) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) h.p[j] = fma(a[i].p[j], h.p[j], u[i].p[j]);
                 if (i < out) put<T, ACC>(y + i * p.y_t, i < n ? h : Four{}, left, false);
@@ -306,22 +413,25 @@ __global__ void __launch_bounds__(THREADS, 3) recur_fwd_k(RecurArgs p, int ranks
         t0 += stride; y += y_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
+    ring.drain(rounds);
     if (CLUSTER) cg::this_cluster().sync();                        // nobody leaves while others may write to its shared memory
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
     if (p.state_out && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.state_out + b * p.C, c0, p.C);
 }
 
 template <typename T, int ACC, int CX, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks, int slices) {
+__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __grid_constant__ Maps maps, int ranks, int slices) {
     const int R = CLUSTER ? ranks : 1;
-    using G = Geo<CX>;
-    using Rg = Ring<T, 3>;
-    extern __shared__ __align__(16) char dyn[];
-    const Rg ring{(typename Rg::V*)dyn + threadIdx.x};
+    using G = Geo<CX, STEPS>;
+    using Rg = Ring<T, ACC, CX, STEPS, 3>;
+    extern __shared__ __align__(128) char dyn[];
+    __shared__ uint64_t full[Rg::STAGES];
+    Rg ring{dyn, full};
     __shared__ __align__(16) float2 tot_h[2][G::TEAMS][G::CH], tot_g[2][G::TEAMS][G::CH];
     __shared__ __align__(16) float own[3][Lane<CX>::ONE ? THREADS * N : 1];
     __shared__ __align__(16) float carried[2][G::CH];
-    __shared__ __align__(16) float2 joined[2][G::RANKS][G::CH];
+    __shared__ __align__(16) Joined<CLUSTER ? G::CH : 2> joined;
+    const Peers<CLUSTER ? G::CH : 2> peers{&joined};
     const int rank = CLUSTER ? (int)(blockIdx.x % R) : 0;
     const long group = blockIdx.x / R, b = group / slices;
     const long c0 = (group - b * slices) * G::CH;
@@ -332,29 +442,21 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
     const int tiles = (T_ + G::TILE - 1) / G::TILE, rounds = (tiles + R - 1) / R, stride = R * G::TILE;
     // rounds go from the end of the sequence to its beginning
     int tile = (rounds - 1) * R + rank, t0 = tile * G::TILE + tg * STEPS, tf = t0;
-    const T* zf = (const T*)p.z + b * p.z_b + c + t0 * p.z_t;
-    const T* vf = (const T*)p.v + b * p.v_b + c + t0 * p.v_t;
-    const T* df = (const T*)p.dy + b * p.dy_b + c + t0 * p.dy_t;
+    const T* gf[3] = {(const T*)p.z + b * p.z_b + c + t0 * p.z_t, (const T*)p.v + b * p.v_b + c + t0 * p.v_t, (const T*)p.dy + b * p.dy_b + c + t0 * p.dy_t};
+    const long step[3] = {p.z_t, p.v_t, p.dy_t}, round_step[3] = {stride * p.z_t, stride * p.v_t, stride * p.dy_t};
     T* dz = (T*)p.dz + b * p.dz_b + c + t0 * p.dz_t;
     T* dv = (T*)p.dv + b * p.dv_b + c + t0 * p.dv_t;
-    const long z_round = stride * p.z_t, v_round = stride * p.v_t, d_round = stride * p.dy_t, dz_round = stride * p.dz_t, dv_round = stride * p.dv_t;
+    const long dz_round = stride * p.dz_t, dv_round = stride * p.dv_t;
     auto fetch_tile = [&](int stage) {
-        const int n = left > 0 && tf >= 0 ? steps_before(len, tf) : 0;
+        if (tf >= 0) ring.fetch(stage, maps, c0, tf - tg * STEPS, b, gf, step, left, steps_before<STEPS>(len, tf));
+        ring.issued();
+        tf -= stride;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-            if (i < n) {
-                fetch<T, ACC>(ring.slot(stage, i, 0), zf + i * p.z_t, left);
-                fetch<T, ACC>(ring.slot(stage, i, 1), vf + i * p.v_t, left);
-                fetch<T, ACC>(ring.slot(stage, i, 2), df + i * p.dy_t, left);
-            } else {
-                idle(ring.slot(stage, i, 0), ring.slot(stage, i, 1));
-                *ring.slot(stage, i, 2) = *ring.slot(stage, i, 1);
-            }
-        copies_issued();
-        tf -= stride; zf -= z_round; vf -= v_round; df -= d_round;
+        for (int q = 0; q < 3; ++q) gf[q] -= round_step[q];
     };
+    ring.begin();
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
-    if (CLUSTER) cg::this_cluster().sync();                        // every CTA is there before anyone writes to its shared memory
+    if (CLUSTER) peers.begin();
     const int first = Lane<CX>::first(), mine = (threadIdx.x & ~31) * N;
     Lane<CX> carry;
     carry.read(p.dstate_out ? p.dstate_out + b * p.C : nullptr, c0, p.C);
@@ -362,26 +464,31 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
     int stage = 0;
     for (int round = 0; round < rounds; ++round) {
         const int now = round & 1;
-        fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);
         Lane<CX> in_h, in_g;
         in_h.read(tile < tiles ? p.saved + ((long)b * tiles + tile) * p.C : nullptr, c0, p.C);
-        copies_arrived<Rg::STAGES - 1>();
+        ring.template arrived<Rg::STAGES - 2>(stage, round);
+        const int n = steps_before<STEPS>(len, t0);
         Four a[STEPS], q[STEPS], A, H, Q;
+        auto look = [&](auto all) {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const Four z = unpack(*ring.slot(stage, i, 0)), v = unpack(*ring.slot(stage, i, 1)), d = unpack(*ring.slot(stage, i, 2));
+            for (int i = 0; i < STEPS; ++i) {
+                Four z = ring.get(stage, 0, i), v = ring.get(stage, 1, i), d = ring.get(stage, 2, i);
+                if (!all.value && i >= n) { idle(z, v); d = v; }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                gate(z.p[j], a[i].p[j], q[i].p[j]);
-                const float2 u = mul(q[i].p[j], v.p[j]);
-                if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u; Q.p[j] = mul(A.p[j], d.p[j]); }
-                else {
-                    H.p[j] = fma(a[i].p[j], H.p[j], u);
-                    A.p[j] = mul(A.p[j], a[i].p[j]);
-                    Q.p[j] = fma(A.p[j], d.p[j], Q.p[j]);        // what dy of this step is in front of the thread's first one
+                for (int j = 0; j < 2; ++j) {
+                    gate(z.p[j], a[i].p[j], q[i].p[j]);
+                    const float2 u = mul(q[i].p[j], v.p[j]);
+                    if (i == 0) { A.p[j] = a[0].p[j]; H.p[j] = u; Q.p[j] = mul(A.p[j], d.p[j]); }
+                    else {
+                        H.p[j] = fma(a[i].p[j], H.p[j], u);
+                        A.p[j] = mul(A.p[j], a[i].p[j]);
+                        Q.p[j] = fma(A.p[j], d.p[j], Q.p[j]);    // what dy of this step is in front of the thread's first one
+                    }
                 }
             }
-        }
+        };
+        if (n == STEPS) look(std::true_type()); else look(std::false_type());
+        if (ring.gave_up) H = Q = {both(NAN), both(NAN)};
         Chain<CX, true> front;                                   // the forward map
         Chain<CX, false> behind;                                 // the backward map
         if constexpr (Lane<CX>::ONE) {
@@ -396,18 +503,18 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
             }
         } else { store(&tot_h[now][team][first], A, H); store(&tot_g[now][team][first], A, Q); }
         __syncthreads();
+        fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);     // where the tile before was: it has been read
         if (CLUSTER) {
-            cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < G::CH) {
                 float ta = 1.f, tq = 0.f;
 #pragma unroll
                 for (int w = G::TEAMS - 1; w >= 0; --w) { const float2 m = tot_g[now][w][threadIdx.x]; tq = fmaf(m.x, tq, m.y); ta *= m.x; }
-                for (int r = 0; r < R; ++r) *cl.map_shared_rank(&joined[now][rank][threadIdx.x], r) = make_float2(ta, tq);
+                peers.send(round, rank, R, ta, tq);
             }
-            cl.sync();
+            if (!ring.gave_up && !peers.arrived(round)) ring.gave_up = true;
             for (int r = R - 1; r >= 0; --r) {
                 if (r == rank) in_g = carry;
-                carry.through(&joined[now][r][first]);
+                carry.through(&joined.at[now][r][first]);
             }
         } else in_g.set(&carried[now][first]);
         for (int w = 0; w < team; ++w) in_h.through(&tot_h[now][w][first]);
@@ -425,13 +532,13 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
         }
 #pragma unroll
         for (int i = 0; i + 1 < STEPS; ++i) {
-            const Four v = unpack(*ring.slot(stage, i, 1));
+            const Four v = ring.get(stage, 1, i);
 #pragma unroll
             for (int j = 0; j < 2; ++j) before[i + 1].p[j] = fma(a[i].p[j], before[i].p[j], mul(q[i].p[j], v.p[j]));
         }
         // one step back: its gradients, and g in front of it
         auto back = [&](int i, Four& oz, Four& ov) {
-            const Four v = unpack(*ring.slot(stage, i, 1)), e = unpack(*ring.slot(stage, i, 2));
+            const Four v = ring.get(stage, 1, i), e = ring.get(stage, 2, i);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float2 d = __fadd2_rn(e.p[j], g.p[j]);
@@ -440,8 +547,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
                 oz.p[j] = mul(mul(a[i].p[j], ov.p[j]), fma(v.p[j], both(-1.f), before[i].p[j]));
             }
         };
-        const int n = left > 0 ? steps_before(len, t0) : 0;
-        if (n == STEPS) {
+        if (n == STEPS && left > 0) {
 #pragma unroll
             for (int i = STEPS - 1; i >= 0; --i) {
                 Four oz, ov;
@@ -450,14 +556,14 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
                 put<T, ACC>(dv + i * p.dv_t, ov, left, p.accum);
             }
         } else {
-            const int out = left > 0 ? steps_before(T_, t0) : 0;
+            const int out = left > 0 ? steps_before<STEPS>(T_, t0) : 0;
 #pragma unroll
             for (int i = STEPS - 1; i >= 0; --i) {
-                Four oz, ov;
-                back(i, oz, ov);
+                Four oz{}, ov{};
+                if (i < n) back(i, oz, ov);
                 if (i < out) {
-                    put<T, ACC>(dz + i * p.dz_t, i < n ? oz : Four{}, left, p.accum);
-                    put<T, ACC>(dv + i * p.dv_t, i < n ? ov : Four{}, left, p.accum);
+                    put<T, ACC>(dz + i * p.dz_t, oz, left, p.accum);
+                    put<T, ACC>(dv + i * p.dv_t, ov, left, p.accum);
                 }
             }
         }
@@ -465,34 +571,72 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, int ranks
         t0 -= stride; tile -= R; dz -= dz_round; dv -= dv_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
+    ring.drain(rounds);
     if (CLUSTER) cg::this_cluster().sync();
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
     if (p.dstate && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.dstate + b * p.C, c0, p.C);
 }
 
-// How a launch is cut: cx threads along the channels, clusters of r CTAs along the steps.  Both directions use the same cut (the states in front of the tiles
-// pass between them), and it depends on the sizes alone.
-struct Cut { int cx, r; };
-Cut cut(long B, long T, long C) {
-    if (T <= 16) return {64, 1};
-    if (T <= 32) return {32, 1};
-    auto tiles = [&](int cx) { return (T + THREADS / cx * STEPS - 1) / (THREADS / cx * STEPS); };
-    auto ctas = [&](int cx) { return B * ((C + N * cx - 1) / (N * cx)); };
-    Cut k{8, 1};
-    if (ctas(8) * MAX_CLUSTER < 2 * 148) k.cx = 4;
-    while (k.r < MAX_CLUSTER && ctas(k.cx) * k.r * 2 <= 2 * 148 && tiles(k.cx) >= 16 * k.r) k.r *= 2;
-    return k;
+// One step from a state to a state, without what a backward pass needs: a thread per channel.  A call for 64 sequences of 1024 channels, in a graph: 3.9 us, 6.3 through the tiles.
+template <typename T>
+__global__ void __launch_bounds__(128) recur_step_k(RecurArgs p) {
+    const long id = (long)blockIdx.x * 128 + threadIdx.x;
+    if (id >= p.B * p.C) return;
+    const long b = id / p.C, c = id - b * p.C;
+    const bool live = !p.lengths || p.lengths[b] > 0;
+    float h = p.state ? p.state[id] : 0.f;
+    if (live) {
+        float2 a, q;
+        gate(both(ld((const T*)p.z + b * p.z_b + c)), a, q);
+        h = fmaf(a.x, h, q.x * ld((const T*)p.v + b * p.v_b + c));
+    }
+    st((T*)p.y + b * p.y_b + c, live ? h : 0.f);
+    if (p.state_out) p.state_out[id] = h;
 }
 
+// How a launch is cut: cx threads along the channels, clusters of r CTAs along the steps.  Both directions use the same cut (the states in front of the tiles
+// pass between them), and it depends on the sizes alone.  The least of a model's times, in us, fitted to 60 measured backward passes (1 to 64 sequences of 48 to 60001
+// steps, 64 to 2048 channels): a round of a CTA takes 1.5 with an SM to itself and 2.4 beside another, 0.6 more in a cluster and a fifth more with a step group
+// per team; a launch 3, with clusters 5; more than two CTAs to an SM come in waves.  Measured, 8 x 2048 x 1024: 39 for (8, 1), 53 for (8, 2) and (4, 1), 109 for (32, 1);
+// 1 x 60001 x 512: 109 for (4, 8), 152 for (8, 8), 412 for (4, 1).
+struct Cut { int cx, r; };
+Cut cut(long B, long T, long C) {
+    Cut best{64, 1};
+    double least = 1e300;
+    for (int cx : {64, 32, 8, 4}) {
+        const long tiles = (T + THREADS / cx * STEPS - 1) / (THREADS / cx * STEPS), groups = B * ((C + N * cx - 1) / (N * cx));
+        for (int r = 1; r <= (cx > 8 ? 1 : MAX_CLUSTER) && (r == 1 || r <= tiles); r *= 2) {
+            const double rounds = (double)((tiles + r - 1) / r), w = (double)groups * r / 148;
+            double round = 1.5 + 0.9 * std::min(1.0, std::max(0.0, w - 1.0));
+            if (cx > 8) round *= 1.2;
+            if (r > 1) round += 0.6;
+            const double us = (r > 1 ? 5 : 3) + (w <= 2 ? rounds * round : std::ceil(w / 2) * (rounds * round + 1));
+            if (us < least - 1e-9) { least = us; best = {cx, r}; }
+        }
+    }
+    return best;
+}
+
+// false: the tensors cannot be described (they are too far apart)
+template <typename T, int CX, int S>
+bool make_maps(const RecurArgs& a, bool back, Maps& m) {
+    using Rg = Ring<T, 16 / (int)sizeof(T), CX, S, 2>;
+    const int dt = sizeof(T) == 2, box = Rg::BOX;
+    return tc::make_map_rows(&m.t[0], dt, a.z, a.C, a.T, a.B, a.z_t, a.z_b, Geo<CX, S>::CH, box) && tc::make_map_rows(&m.t[1], dt, a.v, a.C, a.T, a.B, a.v_t, a.v_b, Geo<CX, S>::CH, box) &&
+           (!back || tc::make_map_rows(&m.t[2], dt, a.dy, a.C, a.T, a.B, a.dy_t, a.dy_b, Geo<CX, S>::CH, box));
+}
 template <typename T, int ACC, int CX, bool BACK, bool CLUSTER>
 cudaError_t launch(const RecurArgs& a, int R, cudaStream_t s) {
-    constexpr int bytes = BACK ? Ring<T, 3>::BYTES : Ring<T, 2>::BYTES;
+    constexpr int S = BACK ? STEPS : STEPS_FWD<T>;
+    using Rg = Ring<T, ACC, CX, S, BACK ? 3 : 2>;
+    Maps maps{};
+    if constexpr (Rg::TMA) if (!make_maps<T, CX, S>(a, BACK, maps)) return launch<T, (sizeof(T) == 2 ? 2 : 1), CX, BACK, CLUSTER>(a, R, s);
     static OncePerDevice once;
     const auto k = BACK ? recur_bwd_k<T, ACC, CX, CLUSTER> : recur_fwd_k<T, ACC, CX, CLUSTER>;
-    const cudaError_t e = allow_smem(once, (const void*)k, bytes);
+    const cudaError_t e = allow_smem(once, (const void*)k, Rg::BYTES);
     if (e != cudaSuccess) return e;
-    const int slices = (int)((a.C + Geo<CX>::CH - 1) / Geo<CX>::CH);
-    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, bytes, s, CLUSTER ? R : 0, a, R, slices);
+    const int slices = (int)((a.C + Geo<CX, S>::CH - 1) / Geo<CX, S>::CH);
+    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, Rg::BYTES, s, CLUSTER ? R : 0, a, maps, R, slices);
 }
 template <typename T, int ACC, bool BACK>
 cudaError_t pick(const RecurArgs& a, cudaStream_t s) {
@@ -504,14 +648,14 @@ cudaError_t pick(const RecurArgs& a, cudaStream_t s) {
         default: return launch<T, ACC, 64, BACK, false>(a, 1, s);
     }
 }
-// elements (4, 2, 1) that may be moved at once: every row of every tensor starts on that many
+// elements that may be moved at once: every row of every tensor starts on that many, and holds a multiple of them
 template <bool BACK>
 cudaError_t run(int dt, const RecurArgs& a, cudaStream_t s) {
     const size_t z = dt ? 2 : 4;
     uint64_t m = (uint64_t)a.C * z | (uintptr_t)a.z | (uintptr_t)a.v | (uint64_t)(a.z_b | a.z_t | a.v_b | a.v_t) * z;
     if (BACK) m |= (uintptr_t)a.dy | (uintptr_t)a.dz | (uintptr_t)a.dv | (uint64_t)(a.dy_b | a.dy_t | a.dz_b | a.dz_t | a.dv_b | a.dv_t) * z;
     else m |= (uintptr_t)a.y | (uint64_t)(a.y_b | a.y_t) * z;
-    if (dt) return m % 8 == 0 ? pick<bf16, 4, BACK>(a, s) : m % 4 == 0 ? pick<bf16, 2, BACK>(a, s) : pick<bf16, 1, BACK>(a, s);
+    if (dt) return m % 16 == 0 ? pick<bf16, 8, BACK>(a, s) : m % 4 == 0 ? pick<bf16, 2, BACK>(a, s) : pick<bf16, 1, BACK>(a, s);
     return m % 16 == 0 ? pick<float, 4, BACK>(a, s) : pick<float, 1, BACK>(a, s);
 }
 
@@ -525,6 +669,10 @@ size_t recur_saved_bytes(int, long B, long T, long C) {
 cudaError_t recur_forward(int dt, const RecurArgs& a, cudaStream_t s) {
     if (a.B * a.C == 0) return cudaSuccess;
     Scope sc(KC_RECUR_FWD, 8.0 * a.B * a.T * a.C, 3.0 * a.B * a.T * a.C * (dt ? 2 : 4), s);
+    if (a.T == 1 && !a.saved) {
+        const unsigned blocks = (unsigned)((a.B * a.C + 127) / 128);
+        return dt ? klaunch(recur_step_k<bf16>, blocks, 128, 0, s, a) : klaunch(recur_step_k<float>, blocks, 128, 0, s, a);
+    }
     return run<false>(dt, a, s);
 }
 

@@ -1639,6 +1639,16 @@ bool make_map_2d(TensorMap* out, const void* base, long inner, long outer, int b
     return r == CUDA_SUCCESS;
 }
 
+bool make_map_rows(TensorMap* out, int dt, const void* base, long C, long T, long B, long t_stride, long b_stride, int box_c, int box_t) {
+    if (!init()) return false;
+    const cuuint64_t z = dt ? 2 : 4;
+    cuuint64_t dims[3] = {(cuuint64_t)C, (cuuint64_t)T, (cuuint64_t)B};
+    cuuint64_t strides[2] = {(cuuint64_t)t_stride * z, (cuuint64_t)b_stride * z};
+    cuuint32_t box[3] = {(cuuint32_t)box_c, (cuuint32_t)box_t, 1}, estr[3] = {1, 1, 1};
+    return g_encode((CUtensorMap*)out, dt ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool pixel_tile(int H, int W, int pixels, int* Wt, int* Ht, int* Nt) {
     auto pow2 = [](int v) { return v > 0 && (v & (v - 1)) == 0; };
     if (!pow2(W) || !pow2(H)) return false;

@@ -56,6 +56,9 @@ bool init();     // resolves the driver's tensor-map encoder; false if unavailab
 // NHWC bf16 tensor [N,H,W,C]; box = boxC channels x (boxW x boxH x boxN) pixels; stride 2 samples every other pixel
 bool make_map_4d(TensorMap* out, const void* base, int C, int W, int H, int N, int boxC, int boxW, int boxH, int boxN, int stride);
 bool make_map_2d(TensorMap* out, const void* base, long inner, long outer, int box_inner, int box_outer);
+// [B][T] rows of C values (dt 0: fp32, 1: bf16), element strides t_stride and b_stride; box = box_c values x box_t rows of one b, dense in shared memory, zeros outside.
+// false: not encodable (addresses and strides have to be multiples of 16 bytes)
+bool make_map_rows(TensorMap* out, int dt, const void* base, long C, long T, long B, long t_stride, long b_stride, int box_c, int box_t);
 // Wt x Ht x Nt = pixels, Wt = min(W, pixels) ...; false unless H and W are powers of two
 bool pixel_tile(int H, int W, int pixels, int* Wt, int* Ht, int* Nt);
 
