@@ -17,6 +17,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fdg {
 namespace {
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ t
     __syncthreads();
     if ((int)blockIdx.x >= sum_ctas) {
         const long ctas = gridDim.x - sum_ctas, per = (vocab + ctas - 1) / ctas, r0 = (blockIdx.x - sum_ctas) * per;
-        fill_rows<256>([&](int i) { return (long)tok_[i]; }, n, dtable, r0, min(vocab, r0 + per), C, N > 1, named);
+        fill_rows<256>([&](int i) { return (long)tok_[i]; }, n, dtable, r0, min(vocab, r0 + per), C, N > 2, named);
         return;
     }
     const int warp = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, i = warp / slices, c = (warp - i * slices) * 32 * N + lane * N;
@@ -402,9 +403,9 @@ __global__ void __launch_bounds__(256) embed_joins_k(int C, float scale, float* 
     }
 }
 
-// elements that may be moved at once
+// elements that may be moved at once: 16 bytes' worth, 2, or 1
 template <typename T> int vector(const void* a, long stride_a, long C) {
-    for (int n = 16 / (int)sizeof(T); n > 1; n = 1) if ((uintptr_t)a % 16 == 0 && stride_a % n == 0 && C % n == 0) return n;
+    for (int n : {16 / (int)sizeof(T), 2}) if ((uintptr_t)a % (n * sizeof(T)) == 0 && stride_a % n == 0 && C % n == 0) return n;
     return 1;
 }
 
@@ -441,6 +442,7 @@ cudaError_t forward_t(const int32_t* tokens, long n, const void* table, long voc
     const int vec = std::min(vector<T>(table, C, C), vector<T>(y, ys, C));
     const int per_row = (int)(C / vec);
     const unsigned blocks = (unsigned)((n * per_row + 256 * UNROLL - 1) / (256 * UNROLL));
+    if (vec == 2) return klaunch(embed_fwd_k<T, 2>, blocks, 256, 0, s, tokens, n, (const T*)table, (unsigned)vocab, (int)C, per_row, scale, (T*)y, ys);
     if (vec == 1) return klaunch(embed_fwd_k<T, 1>, blocks, 256, 0, s, tokens, n, (const T*)table, (unsigned)vocab, (int)C, per_row, scale, (T*)y, ys);
     return klaunch(embed_fwd_k<T, 16 / sizeof(T)>, blocks, 256, 0, s, tokens, n, (const T*)table, (unsigned)vocab, (int)C, per_row, scale, (T*)y, ys);
 }
@@ -463,12 +465,12 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
     cudaError_t e = allow_smem(once, (const void*)embed_sort_k, SORT_WARPS * (1 << MAX_BITS) * (int)sizeof(unsigned));
     if (e != cudaSuccess) return e;
     e = klaunch(embed_sort_k, (unsigned)((vocab + rows - 1) / rows), SORT_THREADS, (size_t)std::max(SORT_WARPS << bits, FILL_ROWS / 32) * sizeof(unsigned), s, tokens, (int)n, vocab,
-                list, other, rows, passes, bits, accum ? nullptr : dtable, (int)C, (int)(N > 1), left.count, left.chains);
+                list, other, rows, passes, bits, accum ? nullptr : dtable, (int)C, (int)(N > 2), left.count, left.chains);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)((p.tiles + 256 / p.tx - 1) / (256 / p.tx)), (unsigned)p.slices);
     e = klaunch(embed_sums_k<T, N>, grid, 256, 0, s, (const uint2*)list, dy, dys, (int)C, scale, (int)accum, dtable, left, p);
     if (e != cudaSuccess || p.tiles == 1) return e;
-    constexpr int J = N > 1 ? 4 : 1;
+    constexpr int J = N > 2 ? 4 : 1;
     const dim3 joins((unsigned)std::min(p.tiles, 8 * 148), (unsigned)((C + J * JOIN_TX - 1) / (J * JOIN_TX)));
     return klaunch(embed_joins_k<J>, joins, 256, 0, s, (int)C, scale, dtable, left, p);
 }
@@ -491,10 +493,14 @@ cudaError_t embed_backward(int dt, const int32_t* tokens, long n, const void* dy
     if (n == 0 && accum) return cudaSuccess;
     Scope sc(KC_EMBED_GRAD, 2.0 * n * C, (double)n * (4 + C * (dt ? 2.0 : 4.0)) + (accum ? 0.0 : 4.0 * vocab * C), s);
     const bool rows = (uintptr_t)dtable % 16 == 0;              // whole vectors of dtable too
-    if (dt) return rows && vector<bf16>(dy, dy_stride, C) > 1 ? backward_t<bf16, 8>(dt, tokens, n, (const bf16*)dy, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s)
-                                                             : backward_t<bf16, 1>(dt, tokens, n, (const bf16*)dy, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s);
-    return rows && vector<float>(dy, dy_stride, C) > 1 ? backward_t<float, 4>(dt, tokens, n, (const float*)dy, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s)
-                                                       : backward_t<float, 1>(dt, tokens, n, (const float*)dy, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s);
+    auto go = [&](auto* p) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
+        const int vec = vector<T>(p, dy_stride, C);
+        if (vec > 2 && rows) return backward_t<T, 16 / sizeof(T)>(dt, tokens, n, p, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s);
+        return vec > 1 ? backward_t<T, 2>(dt, tokens, n, p, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s)
+                       : backward_t<T, 1>(dt, tokens, n, p, dy_stride, vocab, C, scale, accum, dtable, (char*)ws, s);
+    };
+    return dt ? go((const bf16*)dy) : go((const float*)dy);
 }
 
 }  // namespace fdg

@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(128) recur_step_k(RecurArgs p) {
 // pass between them), and it depends on the sizes alone.  The least of a model's times, in us, fitted to 60 measured backward passes (1 to 64 sequences of 48 to 60001
 // steps, 64 to 2048 channels): a round of a CTA takes 1.5 with an SM to itself and 2.4 beside another, 0.6 more in a cluster and a fifth more with a step group
 // per team; a launch 3, with clusters 5; more than two CTAs to an SM come in waves.  Measured, 8 x 2048 x 1024: 39 for (8, 1), 53 for (8, 2) and (4, 1), 109 for (32, 1);
-// 1 x 60001 x 512: 109 for (4, 8), 152 for (8, 8), 412 for (4, 1).
+// 1 x 60001 x 512: 109 for (4, 8), 152 for (8, 8), 412 for (4, 1).  (Clusters of 16 do not all fit on the device at once: 146 for (8, 16).)
 struct Cut { int cx, r; };
 Cut cut(long B, long T, long C) {
     Cut best{64, 1};

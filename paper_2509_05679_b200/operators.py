@@ -102,7 +102,7 @@ def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0, 
     vocab, c = table.shape
     n = tokens.numel()
     if out is None:
-        out = torch.empty((*tokens.shape, c), dtype=dtype, device=dev)
+        out = table.new_empty((*tokens.shape, c))
         stride = c
     else:
         stride = _rows("out", out, dtype, 2, (n, c), dev)
@@ -128,10 +128,10 @@ def embedding_grad(tokens: torch.Tensor, dy: torch.Tensor, vocab: int, *, scale:
     if out is None:
         if accumulate:
             _refuse("accumulate needs the gradient to add to")
-        out = torch.empty((vocab, c), dtype=_F32, device=dev)
+        out = dy.new_empty((vocab, c), dtype=_F32)
     else:
         _dense("out", out, _F32, (vocab, c), dev)
-    ws = torch.empty(need, dtype=_U8, device=dev) if need else None
+    ws = dy.new_empty(need, dtype=_U8) if need else None
     _call(dev, "fdg_embedding_backward", _addr(tokens), n, _addr(dy), _DTYPE[dy.dtype], stride, vocab, c, scale, int(accumulate), _addr(out), _addr(ws), need)
     return out
 
@@ -150,13 +150,13 @@ def recurrence(gate: torch.Tensor, value: torch.Tensor, *, state: Optional[torch
     if lengths is not None:
         _dense("lengths", lengths, _I32, (b,), dev)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=dev)
+        out = gate.new_empty(shape)
         ys = max(n, 1) * c, c
     else:
         ys = _rows("out", out, dtype, 3, shape, dev)
     s = binding.fdg_recurrence(_DTYPE[dtype], b, n, c, *gs, *vs, *ys)
-    last = torch.empty((b, c), dtype=_F32, device=dev)
-    saved = torch.empty(_bytes("fdg_recurrence_saved", C.byref(s)), dtype=_U8, device=dev) if for_grad else None
+    last = gate.new_empty((b, c), dtype=_F32) if state is None else torch.empty_like(state)
+    saved = gate.new_empty(_bytes("fdg_recurrence_saved", C.byref(s)), dtype=_U8) if for_grad else None
     _call(dev, "fdg_recurrence_forward", C.byref(s), _addr(gate), _addr(value), _addr(lengths), _addr(state), _addr(out), _addr(last), _addr(saved))
     return (out, last, saved) if for_grad else (out, last)
 
@@ -178,7 +178,7 @@ def recurrence_grad(gate: torch.Tensor, value: torch.Tensor, dy: torch.Tensor, s
     need = _bytes("fdg_recurrence_saved", C.byref(s))
     if saved.numel() != need:
         _refuse(f"saved must have {need} bytes (those of the forward call of this shape), not {saved.numel()}")
-    first = torch.empty((b, c), dtype=_F32, device=dev)
+    first = gate.new_empty((b, c), dtype=_F32)
     _call(dev, "fdg_recurrence_backward", C.byref(s), _addr(gate), _addr(value), _addr(lengths), _addr(saved), _addr(dy), _addr(dstate), _addr(dgate), _addr(dvalue),
           _addr(first))
     return first
@@ -204,11 +204,11 @@ def distill_loss(logits: torch.Tensor, labels: Optional[torch.Tensor], ids: torc
         if out is not None:
             _refuse("out is for the gradient")
     elif out is None:
-        out, to, ostride = torch.empty((m, v), dtype=dtype, device=dev), dtype, v
+        out, to, ostride = logits.new_empty((m, v)), dtype, v
     else:
         ostride = _rows("out", out, None, 2, (m, v), dev)
         to = out.dtype
-    loss = torch.empty(m, dtype=_F32, device=dev)
+    loss = logits.new_empty(m, dtype=_F32)
     d = binding.fdg_distill(_DTYPE[dtype], _DTYPE[to], ids.shape[1], m, v, stride, ostride, temperature, weight, scale)
     _call(dev, "fdg_distill_loss", C.byref(d), _addr(logits), _addr(labels), _addr(ids), _addr(teacher), _addr(loss), _addr(out))
     return loss, out
