@@ -323,11 +323,12 @@ FDG_API const char* fdg_static_last_error(void);
  *     unless it says so.  Any size works; rows that start on 16 bytes (pointers and strides) are the fast ones.
  *   - A call only enqueues kernels on `stream` (a cudaStream_t, NULL: the default stream): no allocation, no synchronisation, nothing kept between
  *     calls, so it may be captured into a CUDA graph, and calls on different streams, with workspaces of their own, may overlap.
- *   - Arithmetic and sums are in 32 bits, results are rounded once; equal inputs on equal devices give equal bits.
+ *   - Arithmetic and sums are in 32 bits, results are rounded once; equal inputs on equally aligned addresses of equal devices give equal bits.
+ *   - Kernels that wait for copies of their own give up after about two seconds; outputs from there on are NaN.
  *   - A refused call launches nothing; fdg_op_last_error() says why (per thread). */
 
 /* Embedding lookup (the first layer of a token model): out[i] = scale * table[tokens[i]] for i < n.
- *   tokens : int32 [n]; an id outside 0..vocab-1 (padding) gives a row of zeros
+ *   tokens : int32 [n], n <= 2^30; an id outside 0..vocab-1 (padding) gives a row of zeros
  *   table  : [vocab][channels]
  *   out    : n rows of `channels`, out_stride apart */
 FDG_API fdg_status fdg_embedding_forward(const int32_t* dev_tokens, int64_t n, const void* dev_table, int32_t dtype, int64_t vocab, int64_t channels, float scale,
@@ -343,7 +344,7 @@ FDG_API fdg_status fdg_embedding_backward(const int32_t* dev_tokens, int64_t n, 
 /* Gated linear recurrence along the steps of `batch` sequences, every channel by itself:
  *   a_t = sigmoid(gate_t),   h_t = a_t h_{t-1} + (1 - a_t) value_t,   y_t = h_t   (h_0 = state_in, or zero)
  * A single step (steps = 1, state_in, state_out) serves one new token; state_out may be state_in.
- * Tensors are [batch][steps][channels] with strides of their own between sequences and between steps, channels contiguous (so gate and value may be the
+ * Tensors are [batch][steps][channels] (steps <= 2^30, channels <= 2^20) with strides of their own between sequences and between steps, channels contiguous (so gate and value may be the
  * halves of one tensor, or time-major).  state_*, dstate_* are fp32 [batch][channels], contiguous; saved is written by the forward call and read by the
  * backward call of the same shape and dtype (fdg_recurrence_saved bytes, 16-byte aligned).
  *   lengths : int32 [batch] or NULL.  Steps at or behind a sequence's length (clamped to 0..steps) do not count: y is zero there, the gradients are zero,

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(THREADS) distill_warp_k(DistillArgs a) {
         tid[j] = in ? id : -1;
         tp[j] = in ? a.teacher[row * a.k + j] : -INFINITY;
         ts[j] = in ? ld(x + id) : 0.f;
-        tm = fmaxf(tm, tp[j]);
+        tm = fmaxf(tm, tp[j] != tp[j] ? INFINITY : tp[j]);       // (a NaN is not taken for an entry left out)
     }
     for (int v = lane; v < V; v += 32) t.m = fmaxf(t.m, ld(x + v));
     t.m = reduce_warp(t.m, Max()); tm = reduce_warp(tm, Max());
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_row_k(DistillArgs a, int r
                 const bool in = id >= 0 && id < V;
                 tid[j] = in && at >= 0 && at < n * E ? at : -1;
                 tp[j] = in ? raw_t[buf * k + j] : -INFINITY;
-                most[1] = fmaxf(most[1], tp[j]);
+                most[1] = fmaxf(most[1], tp[j] != tp[j] ? INFINITY : tp[j]);     // (a NaN is not taken for an entry left out)
             }
             Top top;
 #pragma unroll 4

@@ -135,7 +135,7 @@ def distill(logits, labels, ids, teacher, tau, weight, scale, grad_dtype):
         inside = (ids >= 0) & (ids < v)
         at = torch.where(inside, ids, 0).long()
         t = torch.where(inside, teacher.to(F64), -torch.inf)
-        taught = (t.amax(1, keepdim=True) > -torch.inf)
+        taught = t.amax(1, keepdim=True) != -torch.inf
         lp = torch.log_softmax(torch.where(taught, t, 0.0) / tau, 1)
         p = torch.where(taught, lp.exp(), 0.0)
         far = (t - t.amax(1, keepdim=True)).abs() / tau

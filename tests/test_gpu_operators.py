@@ -484,6 +484,121 @@ def test_calls_in_graphs_that_share_a_pool(ops):
             assert all(torch.equal(out[k], w[k]) for k in w)
 
 
+def test_first_calls_inside_a_capture(ops):
+    """What a kernel is set up with is set up inside the capture too: rows over a cluster, a sequence over a cluster, many tokens; none of these sizes is used elsewhere."""
+    g = _gen("capture")
+    logits = _normal(g, 5, 70001)
+    ids, teacher = _teacher(g, 5, 70001, 33, "plain")
+    gate, value = _normal(g, 1, 7000, 40, dtype=torch.bfloat16), _normal(g, 1, 7000, 40, dtype=torch.bfloat16)
+    tok, dy = _tokens(g, 5000, 900, "skewed"), _normal(g, 5000, 20, dtype=torch.bfloat16)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [*ops.distill_loss(logits, None, ids, teacher, temperature=1.5), *ops.recurrence(gate, value), ops.embedding_grad(tok, dy, 900)]
+    for t in got:
+        t.fill_(NAN)
+    for _ in range(2):
+        graph.replay()
+    want = [*ops.distill_loss(logits, None, ids, teacher, temperature=1.5), *ops.recurrence(gate, value), ops.embedding_grad(tok, dy, 900)]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    (el, bl), (eg, bg) = ref.distill(logits, None, ids, teacher, 1.5, 1.0, 1.0, torch.float32)
+    ref.check(want[0], el, bl, "loss")
+    ref.check(want[1], eg, bg, "gradient")
+
+
+def test_recurrence_of_broadcast_inputs(ops):
+    """One gate for all sequences, for all steps, and one value for both: strides of zero."""
+    g = _gen("broadcast")
+    b, n, c = 4, 300, 64
+    for dtype in DTYPES:
+        value, dy = _normal(g, b, n, c, dtype=dtype), _normal(g, b, n, c, dtype=dtype)
+        for gate in (_normal(g, 1, n, c, dtype=dtype).expand(b, n, c), _normal(g, b, 1, c, dtype=dtype).expand(b, n, c), _normal(g, 1, 1, c, dtype=dtype).expand(b, n, c)):
+            dx = torch.empty_like(value), torch.empty_like(value)
+            got = _run_recurrence(ops, gate, value, None, None, dy, None, dx)
+            dense = gate.contiguous()
+            dw = torch.empty_like(value), torch.empty_like(value)
+            want = _run_recurrence(ops, dense, value, None, None, dy, None, dw)
+            assert all(torch.equal(p, q) for p, q in zip((*got, *dx), (*want, *dw)))
+            ref.check(got[0], *ref.recurrence(dense, value, None, None)[:2], "y")
+
+
+@pytest.mark.parametrize("b,n,c", [(3, 70, 64), (1, 6000, 72), (2, 1, 40)])
+def test_recurrence_bits_do_not_depend_on_alignment(ops, b, n, c):
+    """Tensor copies, 4-byte copies and single loads see the same tiles."""
+    g = _gen("aligned", b, n, c)
+    for dtype in DTYPES:
+        data = [_normal(g, b, n, c, dtype=dtype) for _ in range(3)]
+        runs = []
+        for off in (0, 2, 1):
+            gate, value, dy = (torch.empty(b * n * c + 8, dtype=dtype, device="cuda")[off:off + b * n * c].view(b, n, c).copy_(t) for t in data)
+            dx = torch.empty_like(gate), torch.empty_like(gate)
+            runs.append((*_run_recurrence(ops, gate, value, None, None, dy, None, dx), *dx))
+        for other in runs[1:]:
+            assert all(torch.equal(p, q) for p, q in zip(runs[0], other))
+
+
+@pytest.mark.parametrize("n", [1, 50, 9000])
+def test_recurrence_updates_a_state_in_place(ops, n):
+    import ctypes
+    from paper_2509_05679_b200 import binding
+    g = _gen("place", n)
+    b, c = 2, 48
+    gate, value, state = _normal(g, b, n, c), _normal(g, b, n, c), _normal(g, b, c)
+    y, last = ops.recurrence(gate, value, state=state)
+    s = binding.fdg_recurrence(0, b, n, c, n * c, c, n * c, c, n * c, c)
+    out = torch.empty_like(y)
+    assert binding.lib().fdg_recurrence_forward(ctypes.byref(s), gate.data_ptr(), value.data_ptr(), None, state.data_ptr(), out.data_ptr(), state.data_ptr(), None, None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, y) and torch.equal(state, last)
+
+
+@pytest.mark.parametrize("v", [40, 3000])
+def test_distillation_of_a_teacher_of_nan(ops, v):
+    """A NaN among a row's entries is the row's; where it is all there is too."""
+    g = _gen("nan", v)
+    logits = _normal(g, 4, v)
+    ids, teacher = _teacher(g, 4, v, 6, "plain")
+    teacher[1, 2] = NAN
+    teacher[2] = NAN
+    loss, grad = ops.distill_loss(logits, None, ids, teacher, temperature=2.0)
+    assert torch.equal(loss.isnan(), torch.tensor([False, True, True, False], device="cuda"))
+    (el, bl), (eg, bg) = ref.distill(logits, None, ids, teacher, 2.0, 1.0, 1.0, torch.float32)
+    ref.check(loss, el, bl, "loss")
+    ref.check(grad[[0, 3]], eg[[0, 3]], bg[[0, 3]], "gradient")
+
+
+def test_embedding_beyond_32_bit_offsets(ops):
+    """A table of more than 2^31 elements and a gradient of more than 2^32 bytes: the last rows."""
+    v, c = (1 << 21) + 5, 1032
+    g = _gen("large")
+    table = torch.zeros(v, c, dtype=torch.bfloat16, device="cuda")
+    table[-8:] = _normal(g, 8, c)
+    for n in (100, 3000):
+        tok = torch.randint(v - 8, v, (n,), generator=g, device="cuda", dtype=torch.int32)
+        y = ops.embedding(tok, table, scale=2.0)
+        assert torch.equal(y, table[tok.long()] * 2)
+        dw = ops.embedding_grad(tok, y, v)
+        exact, bound = ref.embedding_grad(tok - (v - 8), y, 8, 1.0)
+        ref.check(dw[-8:], exact, bound, "dtable")
+        assert not dw[:-8].any()
+        del dw
+
+
+def test_distillation_beyond_32_bit_offsets(ops):
+    m, v = 17000, 131073
+    g = _gen("long")
+    logits = torch.zeros(m, v, dtype=torch.bfloat16, device="cuda")
+    logits[-3:] = _normal(g, 3, v)
+    ids = torch.arange(4, device="cuda", dtype=torch.int32).expand(m, 4).contiguous()
+    teacher = _normal(g, m, 4)
+    loss, grad = ops.distill_loss(logits, None, ids, teacher, out=logits)
+    check = torch.zeros(3, v, dtype=torch.bfloat16, device="cuda")
+    g = _gen("long")
+    check[:] = _normal(g, 3, v)
+    (el, bl), (eg, bg) = ref.distill(check, None, ids[-3:], teacher[-3:], 1.0, 1.0, 1.0, torch.bfloat16)
+    ref.check(loss[-3:], el, bl, "loss")
+    ref.check(grad[-3:], eg, bg, "gradient")
+
+
 def test_refusals_of_tensors(ops):
     """What the host can see to be wrong is refused, and nothing is written."""
     from paper_2509_05679_b200.binding import FdgError
