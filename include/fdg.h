@@ -349,6 +349,7 @@ FDG_API fdg_status fdg_embedding_backward(const int32_t* dev_tokens, int64_t n, 
  * backward call of the same shape and dtype (fdg_recurrence_saved bytes, 16-byte aligned).
  *   lengths : int32 [batch] or NULL.  Steps at or behind a sequence's length (clamped to 0..steps) do not count: y is zero there, the gradients are zero,
  *             whatever gate, value and dy hold; state_out is h after the last step that counts.
+ * A NaN or an infinity in a step that counts leaves NaN or infinities in the steps behind it (backwards: of dy, in front of it) of its sequence and channel, nowhere else.
  * Backward: with d_t = dy_t + a_{t+1} d_{t+1} (and dstate_out added to the last), dvalue_t = (1 - a_t) d_t,
  *   dgate_t = a_t (1 - a_t) d_t (h_{t-1} - value_t), dstate_in = a_1 d_1.  h is computed again in 32 bits from `saved`. */
 typedef struct {
@@ -376,7 +377,7 @@ FDG_API fdg_status fdg_recurrence_backward(const fdg_recurrence* shape, const vo
  *             id count one by one; a row without an entry has no distillation term.  Not read when weight is 0 (may be NULL)
  *   loss    : fp32 [rows]
  *   dlogits : dlogits_dtype, or NULL for the loss alone; may be `logits` itself (same type and stride)
- * Types: logits and dlogits of the same type, or fp32 logits and bf16 dlogits.  vocab <= 262144, top <= 1024, temperature > 0, 0 <= weight <= 1. */
+ * Types: logits and dlogits of the same type, or fp32 logits and bf16 dlogits.  vocab <= 262144, top <= 1024, 1e-6 <= temperature <= 1e6, 0 <= weight <= 1. */
 typedef struct {
     int32_t logits_dtype, dlogits_dtype, top;
     int64_t rows, vocab, logits_stride, dlogits_stride;

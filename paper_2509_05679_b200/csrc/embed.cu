@@ -469,7 +469,7 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)((p.tiles + 256 / p.tx - 1) / (256 / p.tx)), (unsigned)p.slices);
     e = klaunch(embed_sums_k<T, N>, grid, 256, 0, s, (const uint2*)list, dy, dys, (int)C, scale, (int)accum, dtable, left, p);
-    if (e != cudaSuccess || p.tiles == 1) return e;
+    if (e != cudaSuccess) return e;
     constexpr int J = N > 2 ? 4 : 1;
     const dim3 joins((unsigned)std::min(p.tiles, 8 * 148), (unsigned)((C + J * JOIN_TX - 1) / (J * JOIN_TX)));
     return klaunch(embed_joins_k<J>, joins, 256, 0, s, (int)C, scale, dtable, left, p);

@@ -1670,6 +1670,7 @@ fdg_status fdg_create(const fdg_layer* layers, int32_t n_layers, const int32_t* 
         void* p = ctx->alloc.alloc(bytes, ctx->alloc.user);
         if (!p) { oom = true; return nullptr; }
         ctx->blocks.push_back(p); ctx->device_bytes += bytes;
+        ctx->blocks.reserve(ctx->blocks.size() + 1);             // (for fdg_set_distill's, which then need not allocate on the host)
         return (char*)p;
     };
     size_t n_tags = 0;

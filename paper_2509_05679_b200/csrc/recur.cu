@@ -2,7 +2,7 @@
 // Backward, with d_t = dy_t + a_{t+1} d_{t+1}:  dv_t = (1 - a_t) d_t,  dz_t = a_t (1 - a_t) d_t (h_{t-1} - v_t),  dh_0 = a_1 d_1.
 //
 // A step is the affine map h -> a h + u, u = (1 - a) v; maps compose: (A, H) then (A', H') is (A' A, A' H + H').  So a sequence is cut into pieces whose
-// maps are found side by side and joined: a thread composes STEPS = 4 steps of four channels, a warp its threads by shuffles, the CTA its warps and, where
+// maps are found side by side and joined: a thread composes 4 or 8 steps of four channels, a warp its threads through shared memory, the CTA its warps and, where
 // a launch would otherwise be too small, a cluster its CTAs through distributed shared memory; then every thread runs its steps again from the state in front of
 // them.  The joins are a fixed tree, so equal inputs give equal bits.  Backwards the same with g_t = a_t d_t, the map g -> a (g + dy).
 //
@@ -27,11 +27,11 @@ namespace cg = cooperative_groups;
 using bf16 = __nv_bfloat16;
 
 constexpr int THREADS = 256;
-constexpr int STEPS = 4;                // of a thread in a tile, backwards
-// forward, where there are registers for more, and with fp32 no shared memory
+constexpr int STEPS = 4;                // of a thread in a tile, backwards (eight, whose gates would have to be computed twice for want of registers: 52 us instead of 39, 8 x 2048 x 1024)
+// Forward, where there are registers for eight, and with fp32 no shared memory: 1 x 16384 x 2048 bf16 47 us, with four 54; 1 x 60001 x 512: 55 and 62.
 template <typename T> constexpr int STEPS_FWD = sizeof(T) == 2 ? 8 : 4;
 constexpr int N = 4;                    // channels of a thread
-constexpr int MAX_CLUSTER = 8;      // of slices up to 32 channels; wider ones have no clusters
+constexpr int MAX_CLUSTER = 8;          // of slices up to 32 channels; wider ones have no clusters
 
 // CX threads lie along the channels, the others along the steps.
 template <int CX, int S> struct Geo {

@@ -254,6 +254,43 @@ def test_recurrence_of_closed_and_open_gates(ops, dtype):
     assert torch.equal(y[:, :, 2::4], value[:, :, 2::4]) and torch.equal(y[:, :, 3::4], value[:, :, 3::4])
 
 
+@pytest.mark.parametrize("bad", [NAN, float("inf")], ids=str)
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("b,n,c", [(2, 700, 40), (1, 5000, 16), (3, 1100, 300)])
+def test_recurrence_keeps_what_is_not_finite_in_its_channel_and_direction(ops, b, n, c, dtype, bad):
+    """A value that is not finite reaches the steps behind it, a dy the steps in front of it; all others keep their bits."""
+    g = _gen("bad", b, n, c)
+    gate, value, dy = (_normal(g, b, n, c, dtype=dtype) for _ in range(3))
+
+    def passes(value, dy):
+        y, last, saved = ops.recurrence(gate, value, for_grad=True)
+        dgate, dvalue = torch.empty_like(gate), torch.empty_like(gate)
+        first = ops.recurrence_grad(gate, value, dy, saved, dgate=dgate, dvalue=dvalue)
+        return y, last, dgate, dvalue, first
+    clean = passes(value, dy)
+    s, t, k = b - 1, n // 3, c // 2
+    spoilt = value.clone()
+    spoilt[s, t, k] = bad
+    y, last, dgate, dvalue, first = passes(spoilt, dy)
+    assert not y[s, t:, k].isfinite().any() and not last[s, k].isfinite() and not dgate[s, t:, k].isfinite().any()
+    for got, want in zip((y, last, dgate, dvalue, first), clean):
+        if got.dim() == 3 and got is not dvalue:
+            got[s, t:, k] = want[s, t:, k]
+        elif got is last:
+            got[s, k] = want[s, k]
+        assert torch.equal(got, want)
+    spoilt = dy.clone()
+    spoilt[s, t, k] = bad
+    y, last, dgate, dvalue, first = passes(value, spoilt)
+    assert not dvalue[s, :t + 1, k].isfinite().any() and not first[s, k].isfinite()
+    for got, want in zip((y, last, dgate, dvalue, first), clean):
+        if got is dgate or got is dvalue:
+            got[s, :t + 1, k] = want[s, :t + 1, k]
+        elif got is first:
+            got[s, k] = want[s, k]
+        assert torch.equal(got, want)
+
+
 def test_recurrence_step_by_step_continues_a_sequence(ops):
     """Single steps from the carried state, the state updated in place."""
     g = _gen("steps")
