@@ -428,7 +428,10 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
     __shared__ uint64_t full[Rg::STAGES];
     Rg ring{dyn, full};
     __shared__ __align__(16) float2 tot_h[2][G::TEAMS][G::CH], tot_g[2][G::TEAMS][G::CH];
-    __shared__ __align__(16) float own[3][Lane<CX>::ONE ? THREADS * N : 1];
+    // A warp's maps.  fp32: where its gates were in the tile, which nobody needs any more (a room of their own would leave one CTA to an SM: 8 x 2048 x 1024 78 us instead of 57)
+    constexpr bool IN_TILE = Lane<CX>::ONE && sizeof(T) == 4;
+    static_assert(!IN_TILE || 3 * sizeof(float) <= STEPS * sizeof(T), "three maps' values a thread and channel lie in its gates' place");
+    __shared__ __align__(16) float room[3][Lane<CX>::ONE && !IN_TILE ? THREADS * N : 1];
     __shared__ __align__(16) float carried[2][G::CH];
     __shared__ __align__(16) Joined<CLUSTER ? G::CH : 2> joined;
     const Peers<CLUSTER ? G::CH : 2> peers{&joined};
@@ -457,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
     ring.begin();
     for (int s = 0; s < Rg::STAGES - 1; ++s) fetch_tile(s);
     if (CLUSTER) peers.begin();
-    const int first = Lane<CX>::first(), mine = (threadIdx.x & ~31) * N;
+    const int first = Lane<CX>::first(), at = (threadIdx.x & 31) * N;
     Lane<CX> carry;
     carry.read(p.dstate_out ? p.dstate_out + b * p.C : nullptr, c0, p.C);
     if (threadIdx.x < G::CH) carried[0][threadIdx.x] = p.dstate_out && c0 + threadIdx.x < p.C ? p.dstate_out[b * p.C + c0 + threadIdx.x] : 0.f;
@@ -489,19 +492,24 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         };
         if (n == STEPS) look(std::true_type()); else look(std::false_type());
         if (ring.gave_up) H = Q = {both(NAN), both(NAN)};
+        float* own[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            own[k] = IN_TILE ? (float*)(dyn + stage * Rg::STAGE + (threadIdx.x >> 5) * (32 * N * STEPS * (int)sizeof(T))) + k * 32 * N : &room[k][(threadIdx.x & ~31) * N];
         Chain<CX, true> front;                                   // the forward map
         Chain<CX, false> behind;                                 // the backward map
         if constexpr (Lane<CX>::ONE) {
             __syncwarp();
-            store(&own[0][threadIdx.x * N], A); store(&own[1][threadIdx.x * N], H); store(&own[2][threadIdx.x * N], Q);
+            store(own[0] + at, A); store(own[1] + at, H); store(own[2] + at, Q);
             __syncwarp();
-            front.read(&own[0][mine], &own[1][mine]);
-            behind.read(&own[0][mine], &own[2][mine]);
+            front.read(own[0], own[1]);
+            behind.read(own[0], own[2]);
             if (Lane<CX>::writes()) {
                 tot_h[now][team][first] = make_float2(front.ta, front.th);
                 tot_g[now][team][first] = make_float2(behind.ta, behind.th);
             }
         } else { store(&tot_h[now][team][first], A, H); store(&tot_g[now][team][first], A, Q); }
+        if (IN_TILE && Rg::TMA) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the tile before was written to; a tensor copy is about to
         __syncthreads();
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);     // where the tile before was: it has been read
         if (CLUSTER) {
@@ -521,11 +529,11 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         for (int w = G::TEAMS - 1; w > team; --w) in_g.through(&tot_g[now][w][first]);
         Four g, before[STEPS];
         if constexpr (Lane<CX>::ONE) {
-            front.apply(in_h.v[0], &own[1][mine]);
-            behind.apply(in_g.v[0], &own[2][mine]);
+            front.apply(in_h.v[0], own[1]);
+            behind.apply(in_g.v[0], own[2]);
             __syncwarp();
-            before[0] = load(&own[1][threadIdx.x * N]);
-            g = load(&own[2][threadIdx.x * N]);
+            before[0] = load(own[1] + at);
+            g = load(own[2] + at);
         } else {
             before[0] = {make_float2(in_h.v[0], in_h.v[1]), make_float2(in_h.v[2], in_h.v[3])};
             g = {make_float2(in_g.v[0], in_g.v[1]), make_float2(in_g.v[2], in_g.v[3])};

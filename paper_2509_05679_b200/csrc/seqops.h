@@ -1,6 +1,6 @@
 // Operators on token sequences: embedding lookup, gated linear recurrence, distillation loss.  Launch interface shared by the C entry points on a
 // caller's tensors (op_api.cu) and the step executor (fdg_api.cu).  Device pointers, `dt` 0: fp32, 1: bf16; sizes are checked by the callers.
-// Every function returns the first launch error (and leaves none behind).
+// Every function returns the first error of its launches; the runtime keeps it too, which is where the step executor asks.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
