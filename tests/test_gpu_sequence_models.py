@@ -75,7 +75,9 @@ def test_one_stream_worker_groups_and_many_streams_agree():
     for kw in (dict(grid_sms=148), dict(serial=True, grid_sms=148), dict(worker_groups=4, grid_sms=148)):
         ctx = make_ctx(net, p0, **kw)
         for t in range(12):
-            ctx.step(binding.to_device("bf16", sy.batch_inputs(net, t)), torch.from_numpy(sy.batch_labels(net, t)).cuda())
+            x, y = binding.to_device("bf16", sy.batch_inputs(net, t)), torch.from_numpy(sy.batch_labels(net, t)).cuda()
+            ctx.step(x, y)
+            ctx.wait_ingest()       # from here on their memory may become the next batch's
         out.append(ctx.params())
         ctx.close()
     assert np.array_equal(out[0], out[1])
