@@ -4,7 +4,7 @@
 //
 // The gradient's sums are made in the order of the tokens' positions (in pieces of fixed size), never by atomic additions, so that equal inputs give equal bits.
 // Few tokens: a warp per token looks through all of them.  Otherwise the positions are sorted by token (stable) and the sorted list is cut into tiles:
-//   sort    every CTA owns a range of the table's rows: it picks the tokens of its range out of all (and counts the smaller ones, so it knows its place in the
+//   sort    every CTA owns a share of the table's rows: it picks their tokens out of all (and counts those of the CTAs in front, so it knows its place in the
 //           list without asking anyone), sorts them, and fills the rows that none names with zeros.  Reading all tokens in every CTA costs 1 us per 8000;
 //           a cluster that sorted for all took 56 us for 131072 tokens, this 28.  (All rows filled from the start, beside the sort: 112 instead of 104 us for
 //           131072 rows of 1024, of which 46000 occur; HBM takes writes alone at 4.8 to 5.5 TB/s, so those that are written anyway are better left out.)
@@ -76,31 +76,32 @@ __global__ void __launch_bounds__(256) embed_fwd_k(const int32_t* __restrict__ t
     }
 }
 
-// Zeros to the rows [r0, r1) of dtable that none of n tokens names, by a CTA of THREADS.  Written rows are the bound, so those that the sums write are left
-// out: the CTA marks the rows of its range that occur.
+// Zeros to those of `rows` rows of dtable that none of n tokens names, by a CTA of THREADS.  token(i): the row of token i, counted from 0 (negative or behind: not one of these);
+// place(r): where row r is in dtable, at or behind vocab: nowhere.  Written rows are the bound, so those that the sums write are left out: the CTA marks the rows that occur.
 constexpr int FILL_ROWS = 8192;                 // that it looks at a time
-template <int THREADS, typename Tokens>
-__device__ __forceinline__ void fill_rows(Tokens token, int n, float* dtable, long r0, long r1, int C, bool vec, unsigned* named) {
-    for (long b = r0; b < r1; b += FILL_ROWS) {
-        const int rows = (int)min((long)FILL_ROWS, r1 - b);
+template <int THREADS, typename Tokens, typename Place>
+__device__ __forceinline__ void fill_rows(Tokens token, int n, float* dtable, long rows, long vocab, Place place, int C, bool vec, unsigned* named) {
+    for (long b = 0; b < rows; b += FILL_ROWS) {
+        const int now = (int)min((long)FILL_ROWS, rows - b);
         __syncthreads();
-        for (int i = threadIdx.x; i < (rows + 31) / 32; i += THREADS) named[i] = 0;
+        for (int i = threadIdx.x; i < (now + 31) / 32; i += THREADS) named[i] = 0;
         __syncthreads();
 #pragma unroll 8
         for (int i = threadIdx.x; i < n; i += THREADS) {
             const long t = token(i) - b;                        // (common tokens: one atomic operation, not thousands at one address)
-            if (t >= 0 && t < rows && !(((volatile unsigned*)named)[t >> 5] >> (t & 31) & 1)) atomicOr(&named[t >> 5], 1u << (t & 31));
+            if (t >= 0 && t < now && !(((volatile unsigned*)named)[t >> 5] >> (t & 31) & 1)) atomicOr(&named[t >> 5], 1u << (t & 31));
         }
         __syncthreads();
         const unsigned per = vec ? C / 4 : C;
-        float* d = dtable + b * C;
         unsigned row = threadIdx.x / per, col = threadIdx.x - row * per;
         const unsigned row_step = THREADS / per, col_step = THREADS - row_step * per;
-        d += (long)threadIdx.x * (vec ? 4 : 1);
 #pragma unroll 4
-        for (; row < (unsigned)rows;) {
-            if (!(named[row >> 5] >> (row & 31) & 1)) { if (vec) *(float4*)d = make_float4(0.f, 0.f, 0.f, 0.f); else *d = 0.f; }
-            d += THREADS * (vec ? 4 : 1);
+        for (; row < (unsigned)now;) {
+            const long at = place(b + row);
+            if (at < vocab && !(named[row >> 5] >> (row & 31) & 1)) {
+                float* const d = dtable + at * C;
+                if (vec) ((float4*)d)[col] = make_float4(0.f, 0.f, 0.f, 0.f); else d[col] = 0.f;
+            }
             row += row_step; col += col_step;
             if (col >= per) { col -= per; ++row; }
         }
@@ -108,6 +109,8 @@ __device__ __forceinline__ void fill_rows(Tokens token, int n, float* dtable, lo
 }
 
 // ---- gradient of few tokens, in one launch
+// Sorted, 512 ids of 32000 x 1024 take 38 us instead of 26 (1000 x 128: 17 instead of 6), 2048 take 39 instead of 38; the more equal ones there are, the longer a warp adds: where three in
+// ten are one id, 512 take 60 (27), sorted 37 (17).
 constexpr int FEW = 512;
 // CTAs 0 .. sum_ctas - 1: a warp per token and 32 N channels; it goes on if no earlier token is the same, and adds up all that are, in order.  The
 // others fill the rows that no token names.
@@ -121,7 +124,7 @@ __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ t
     __syncthreads();
     if ((int)blockIdx.x >= sum_ctas) {
         const long ctas = gridDim.x - sum_ctas, per = (vocab + ctas - 1) / ctas, r0 = (blockIdx.x - sum_ctas) * per;
-        fill_rows<256>([&](int i) { return (long)tok_[i]; }, n, dtable, r0, min(vocab, r0 + per), C, N > 2, named);
+        fill_rows<256>([&](int i) { return (long)tok_[i] - r0; }, n, dtable, min(vocab - r0, per), vocab, [&](long r) { return r0 + r; }, C, N > 2, named);
         return;
     }
     const int warp = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, i = warp / slices, c = (warp - i * slices) * 32 * N + lane * N;
@@ -135,6 +138,23 @@ __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ t
     float sum[N] = {};
     for (int j = i; j < n; j += 32) {
         unsigned hits = __ballot_sync(~0u, j + lane < n && tok_[j + lane] == tok);
+        auto add = [&](const Raw<T, N>& row) {
+            float x[N];
+            unpack<T, N>(row, x);
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] += x[k];
+        };
+        if (hits == ~0u) {                                      // one id everywhere
+            if (in)
+                for (int q = 0; q < 32; q += 16) {
+                    Raw<T, N> r[16];
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) r[u] = *(const Raw<T, N>*)(dy + (long)(j + q + u) * dys + c);
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) add(r[u]);
+                }
+            hits = 0;
+        }
         while (hits) {
             Raw<T, N> r[4];
             int m = 0;
@@ -143,12 +163,7 @@ __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ t
                 if (hits) { const int q = __ffs(hits) - 1; hits &= hits - 1; m = u + 1; if (in) r[u] = *(const Raw<T, N>*)(dy + (j + q) * dys + c); }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (u < m && in) {
-                    float x[N];
-                    unpack<T, N>(r[u], x);
-#pragma unroll
-                    for (int k = 0; k < N; ++k) sum[k] += x[k];
-                }
+                if (u < m && in) add(r[u]);
         }
     }
     if (!in) return;
@@ -158,7 +173,8 @@ __global__ void __launch_bounds__(256) embed_few_k(const int32_t* __restrict__ t
 }
 
 // ---- gradient of many tokens
-constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CTAS = 148, MAX_BITS = 10;
+constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_BITS = 10;
+constexpr int OWNER_BITS = 7, OWNERS = 1 << OWNER_BITS;
 
 // the lanes whose d is this one's, by ballots: __match_any_sync takes longer for 32 different values (a sort 89 us instead of 56)
 __device__ __forceinline__ unsigned equals(unsigned d, int bits) {
@@ -167,14 +183,21 @@ __device__ __forceinline__ unsigned equals(unsigned d, int bits) {
     return m;
 }
 
-// The list: entries {token, position} by token, then position; tokens outside the table are not in it.  *count: its length.
-__global__ void __launch_bounds__(SORT_THREADS, 1) embed_sort_k(const int32_t* __restrict__ tokens, int n, long vocab, uint2* list, uint2* other, long rows, int passes, int bits,
+// A CTA owns every 128th group of 2^gs rows of the table: frequent tokens often have small ids, and with a range each (128 times as many rows in a row) the first CTA would sort most of
+// them: 131072 ids whose frequency falls like 1 / id, 131072 rows of 1024, 219 us instead of 378; a million, 32000 rows of 64, 382 instead of 1183.  An owner's rows are counted from 0.
+__device__ __forceinline__ unsigned owner_of(unsigned token, int gs) { return token >> gs & (OWNERS - 1); }
+__device__ __forceinline__ unsigned row_in(unsigned token, int gs) { return token >> (OWNER_BITS + gs) << gs | (token & ((1u << gs) - 1)); }
+__device__ __forceinline__ long row_of(unsigned row, unsigned owner, int gs) { return ((long)(row >> gs) << OWNER_BITS | owner) << gs | (row & ((1u << gs) - 1)); }
+
+// The list: entries {token, position} by owner, then token, then position; tokens outside the table are not in it.  *count: its length.
+__global__ void __launch_bounds__(SORT_THREADS, 1) embed_sort_k(const int32_t* __restrict__ tokens, int n, unsigned vocab, uint2* list, uint2* other, int rows, int gs, int passes, int bits,
                                                                float* dtable, int C, int vec, unsigned* count, unsigned* chains) {
     extern __shared__ unsigned hist[];                          // [warp][bin]
     __shared__ unsigned sums[SORT_WARPS], less[SORT_WARPS];
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long first = blockIdx.x * rows, last = min(vocab, first + rows);
-    const unsigned r0 = (unsigned)first, span = (unsigned)(last - first);
+    const unsigned self = blockIdx.x;
+    auto is_mine = [&](unsigned t) { return t < vocab && owner_of(t, gs) == self; };
+    auto is_less = [&](unsigned t) { return t < vocab && owner_of(t, gs) < self; };
     const bool aligned = (uintptr_t)tokens % 16 == 0;
     // tokens of the warp, 128 at a time, four consecutive ones a lane, to f(first position, the four)
     const int per_warp = (int)(((n + SORT_WARPS - 1l) / SORT_WARPS + 127) / 128 * 128);
@@ -193,26 +216,26 @@ __global__ void __launch_bounds__(SORT_THREADS, 1) embed_sort_k(const int32_t* _
             for (int u = 0; u < AHEAD; ++u) if (i0 + u * 128 < end) f(i0 + u * 128 + lane * 4, t[u]);
         }
     };
-    // how many are smaller than the range, how many are the warp's in it
+    // how many have an earlier owner, how many are the warp's of this one
     unsigned mine = 0, smaller = 0;
     each([&](int, const uint4& t) {
-        mine += (t.x - r0 < span) + (t.y - r0 < span) + (t.z - r0 < span) + (t.w - r0 < span);
-        smaller += (t.x < r0) + (t.y < r0) + (t.z < r0) + (t.w < r0);
+        mine += is_mine(t.x) + is_mine(t.y) + is_mine(t.z) + is_mine(t.w);
+        smaller += is_less(t.x) + is_less(t.y) + is_less(t.z) + is_less(t.w);
     });
     mine = __reduce_add_sync(~0u, mine); smaller = __reduce_add_sync(~0u, smaller);
     if (lane == 0) { sums[w] = mine; less[w] = smaller; }
     __syncthreads();
-    unsigned at = 0, m = 0, base = 0;                           // the warp's place, the range's entries, its place in the list
+    unsigned at = 0, m = 0, base = 0;                           // the warp's place, the owner's entries, its place in the list
     for (int q = 0; q < SORT_WARPS; ++q) { if (q < w) at += sums[q]; m += sums[q]; base += less[q]; }
     if (threadIdx.x == 0) {
-        if (last == vocab) *count = base + m;
+        if (self == gridDim.x - 1) *count = base + m;
         if (blockIdx.x == 0) *chains = 0;
     }
-    // the range's entries, in order
+    // the owner's entries, in order
     uint2* src = (passes & 1 ? other : list) + base;
     uint2* dst = (passes & 1 ? list : other) + base;
     each([&](int i, const uint4& t) {
-        const bool a = t.x - r0 < span, b = t.y - r0 < span, c = t.z - r0 < span, d = t.w - r0 < span;
+        const bool a = is_mine(t.x), b = is_mine(t.y), c = is_mine(t.z), d = is_mine(t.w);
         if (!__any_sync(~0u, a || b || c || d)) return;
         const unsigned A = __ballot_sync(~0u, a), B = __ballot_sync(~0u, b), Cc = __ballot_sync(~0u, c), D = __ballot_sync(~0u, d), lt = (1u << lane) - 1;
         unsigned to = at + __popc(A & lt) + __popc(B & lt) + __popc(Cc & lt) + __popc(D & lt);
@@ -223,19 +246,28 @@ __global__ void __launch_bounds__(SORT_THREADS, 1) embed_sort_k(const int32_t* _
         at += __popc(A) + __popc(B) + __popc(Cc) + __popc(D);
     });
     __syncthreads();
-    // sorted by `bits` bits of the row in the range a pass; a warp has a run of the entries and counts of its own
+    // sorted by `bits` bits of the owner's row a pass; a warp has a run of the entries and counts of its own, and AHEAD times 32 of them on their way
     const int bins = 1 << bits, run = (int)((m + SORT_THREADS - 1) / SORT_THREADS * 32);
     const int lo = (int)min((long)m, (long)w * run), hi = (int)min((long)m, (long)(w + 1) * run);
     unsigned* const own = hist + w * bins;
+    constexpr int AHEAD = 4;
     for (int p = 0; p < passes; ++p) {
         const int shift = p * bits;
         for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_THREADS) hist[i] = 0;
         __syncthreads();
-        for (int i = lo; i < hi; i += 32) {
-            const bool in = i + lane < hi;
-            const unsigned d = in ? (__ldcg(&src[i + lane].x) - r0) >> shift & (bins - 1) : 0, peers = equals(d, bits) & __ballot_sync(~0u, in);
-            if (in && lane == __ffs(peers) - 1) own[d] += __popc(peers);
-            __syncwarp();
+        for (int i0 = lo; i0 < hi; i0 += 32 * AHEAD) {
+            unsigned t[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) { const int i = i0 + u * 32 + lane; t[u] = i < hi ? __ldcg(&src[i].x) : 0; }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int i = i0 + u * 32;
+                if (i >= hi) break;
+                const bool in = i + lane < hi;
+                const unsigned d = row_in(t[u], gs) >> shift & (bins - 1), peers = equals(d, bits) & __ballot_sync(~0u, in);
+                if (in && lane == __ffs(peers) - 1) own[d] += __popc(peers);
+                __syncwarp();
+            }
         }
         __syncthreads();
         // where every warp's part of every bin begins
@@ -255,21 +287,28 @@ __global__ void __launch_bounds__(SORT_THREADS, 1) embed_sort_k(const int32_t* _
 #pragma unroll 8
             for (int q = 0; q < SORT_WARPS; ++q) hist[q * bins + b] += before;
         __syncthreads();
-        for (int i = lo; i < hi; i += 32) {
-            const bool in = i + lane < hi;
-            const uint2 e = in ? __ldcg(src + i + lane) : make_uint2(r0, 0);
-            const unsigned d = (e.x - r0) >> shift & (bins - 1), peers = equals(d, bits) & __ballot_sync(~0u, in), to = own[d];
-            __syncwarp();
-            if (in) {
-                if (lane == __ffs(peers) - 1) own[d] = to + __popc(peers);
-                dst[to + __popc(peers & ((1u << lane) - 1))] = e;
+        for (int i0 = lo; i0 < hi; i0 += 32 * AHEAD) {
+            uint2 e[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) { const int i = i0 + u * 32 + lane; e[u] = i < hi ? __ldcg(src + i) : make_uint2(0, 0); }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int i = i0 + u * 32;
+                if (i >= hi) break;
+                const bool in = i + lane < hi;
+                const unsigned d = row_in(e[u].x, gs) >> shift & (bins - 1), peers = equals(d, bits) & __ballot_sync(~0u, in), to = own[d];
+                __syncwarp();
+                if (in) {
+                    if (lane == __ffs(peers) - 1) own[d] = to + __popc(peers);
+                    dst[to + __popc(peers & ((1u << lane) - 1))] = e[u];
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
         __syncthreads();
         uint2* const t = src; src = dst; dst = t;
     }
-    if (dtable) fill_rows<SORT_THREADS>([&](int i) { return (long)__ldcg(&src[i].x); }, (int)m, dtable, first, last, C, vec, hist);
+    if (dtable) fill_rows<SORT_THREADS>([&](int i) { return (long)row_in(__ldcg(&src[i].x), gs); }, (int)m, dtable, rows, vocab, [&](long r) { return row_of((unsigned)r, self, gs); }, C, vec, hist);
 }
 
 // How the sorted list is cut: tiles of `tile` entries, each summed by teams of `tx` threads (of which `slices` cover the channels).
@@ -416,9 +455,12 @@ Plan plan(int dt, long n, long C, int vec) {
     Plan p;
     const int most = dt ? 8 : 4;
     const long threads = (C + most - 1) / most;                 // of a tile, with whole vectors
-    // tiles: enough teams for a quarter of the device's threads, of 16 to 128 entries (longer ones leave fewer partial rows to join, and fewer teams)
+    // Tiles: the shortest whose teams the device holds at once (three CTAs an SM), or, where even the longest are more, 32: many short waves instead of a little more than one.
+    // 16384 x 1024 bf16 in tiles of 16, 32, 64, 128: 55, 49, 51, 68 us; 131072 x 1024: 205, 191, 193, 218; 131072 x 256: 69, 63, 59, 67; a million x 64: 275, 259, 236, 216.
+    const long room = 148l * 3 * 256;
     int t = 16;
-    while (t < 128 && (n / (2 * t)) * threads >= 148l * 512) t *= 2;
+    while (t < 128 && (n + t - 1) / t * threads > room) t *= 2;
+    if ((n + t - 1) / t * threads > room) t = 32;
     p.tile = t;
     p.tiles = (int)((n + t - 1) / t);
     p.tx = 1 << std::min(8, log2_up((C + vec - 1) / vec));
@@ -459,13 +501,14 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
     uint2 *const list = (uint2*)ws, *const other = (uint2*)(ws + sp.list);
     unsigned* const counts = (unsigned*)(ws + sp.chain);
     const Left left{(float*)(ws + sp.part), (int*)(ws + sp.head), counts, counts + 1, (int2*)(counts + 2)};
-    const long rows = (vocab + SORT_CTAS - 1) / SORT_CTAS;
+    const int gs = log2_up((32 + C - 1) / C);                    // a group: 128 bytes of the table at least
+    const long groups = ((vocab - 1) >> gs) + 1, rows = ((groups + OWNERS - 1) >> OWNER_BITS) << gs;      // rows of an owner, the last of which may be behind the table
     const int key_bits = std::max(1, log2_up(rows)), passes = (key_bits + MAX_BITS - 1) / MAX_BITS, bits = (key_bits + passes - 1) / passes;
     static OncePerDevice once;
     cudaError_t e = allow_smem(once, (const void*)embed_sort_k, SORT_WARPS * (1 << MAX_BITS) * (int)sizeof(unsigned));
     if (e != cudaSuccess) return e;
-    e = klaunch(embed_sort_k, (unsigned)((vocab + rows - 1) / rows), SORT_THREADS, (size_t)std::max(SORT_WARPS << bits, FILL_ROWS / 32) * sizeof(unsigned), s, tokens, (int)n, vocab,
-                list, other, rows, passes, bits, accum ? nullptr : dtable, (int)C, (int)(N > 2), left.count, left.chains);
+    e = klaunch(embed_sort_k, (unsigned)std::min<long>(groups, OWNERS), SORT_THREADS, (size_t)std::max(SORT_WARPS << bits, FILL_ROWS / 32) * sizeof(unsigned), s, tokens, (int)n, (unsigned)vocab,
+                list, other, (int)rows, gs, passes, bits, accum ? nullptr : dtable, (int)C, (int)(N > 2), left.count, left.chains);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)((p.tiles + 256 / p.tx - 1) / (256 / p.tx)), (unsigned)p.slices);
     e = klaunch(embed_sums_k<T, N>, grid, 256, 0, s, (const uint2*)list, dy, dys, (int)C, scale, (int)accum, dtable, left, p);
