@@ -78,9 +78,10 @@ struct Terms {
     }
 };
 
-// ---- a warp per row: small vocabularies, where the row comes out of L1 in the later passes
-constexpr long WARP_VOCAB = 1024;
+// ---- a warp per row: small vocabularies, where the row comes out of L1 in the later passes.  Its time grows with the vocabulary, a CTA's with its rows (444 CTAs are there at once, a row
+// takes 3.4 us).  bf16, warp and CTA: 200 rows of 512 6.3 and 6.3 us, of 1000 10.3 and 6.3; 1776 rows of 1000 12.4 and 16.5, of 2000 16.5 and 18.5, of 4000 39 and 21; 8192 rows of 2000 46 and 65.
 constexpr int WARP_TOP = 128;
+bool warp_per_row(long M, long V, int k) { return k <= WARP_TOP && (V <= 512 || (V <= 2048 && M * 512 >= 444 * V)); }
 template <typename TI, typename TO, int SQ, bool HARD>
 __global__ void __launch_bounds__(THREADS) distill_warp_k(DistillArgs a) {
     __shared__ float tp_[WARPS][WARP_TOP], ts_[WARPS][WARP_TOP];
@@ -450,10 +451,10 @@ struct Resident {
 
 template <typename TI, typename TO, int SQ, bool HARD>
 cudaError_t launch(const DistillArgs& a, cudaStream_t s) {
-    if (a.V <= WARP_VOCAB && a.k <= WARP_TOP)
+    if (warp_per_row(a.M, a.V, a.k))
         return klaunch(distill_warp_k<TI, TO, SQ, HARD>, (unsigned)((a.M + WARPS - 1) / WARPS), THREADS, 0, s, a);
     // A CTA's share of a row: up to 100 KB, so that two fit on an SM (three up to 64 KB) and one copies while others compute; smaller where there are too few rows for
-    // the SMs, down to 16 KB.  1500 rows of 100003 fp32 logits: 271 us in four shares, 327 in eight (more time in the cluster's barriers), 295 in four with 512 threads
+    // the SMs, down to 16 KB (8 rows of 32000 bf16 8.3 us, 10.4 in one share each).  1500 rows of 100003 fp32 logits: 271 us in four shares, 327 in eight (more time in the cluster's barriers), 295 in four with 512 threads
     // a CTA (more time in the joins).
     constexpr int E = Chunk<TI>::E;
     const long chunks = (a.V + E - 1) / E + 1;      // with one more for a row that starts inside a chunk

@@ -53,7 +53,7 @@ def _tokens(g, n, vocab, kind):
 # ---- embedding
 
 EMBED = [(1, 1, 1), (1, 10, 8), (5, 3, 7), (33, 1000, 100), (64, 2, 64), (257, 70001, 24), (512, 9000, 36), (513, 1, 5), (1000, 50, 129), (2100, 300, 40), (700, 128, 1024),
-         (300, 37, 2050), (1025, 148, 12), (1537, 149, 3)]
+         (300, 37, 2050), (1025, 148, 12), (1537, 149, 3), (9001, 40, 4)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)
@@ -335,7 +335,7 @@ def test_recurrence_beyond_32_bit_offsets(ops):
 
 # ---- distillation
 
-DISTILL = [(1, 1, 1), (3, 2, 2), (4, 10, 4), (130, 10, 4), (7, 33, 1), (6, 1000, 20), (5, 1025, 300), (3, 4099, 64), (9, 32000, 64), (2, 50257, 8), (3, 100003, 1000), (2, 262144, 5)]
+DISTILL = [(900, 800, 17), (1800, 2000, 9), (1, 1, 1), (3, 2, 2), (4, 10, 4), (130, 10, 4), (7, 33, 1), (6, 1000, 20), (5, 1025, 300), (3, 4099, 64), (9, 32000, 64), (2, 50257, 8), (3, 100003, 1000), (2, 262144, 5)]
 
 
 def _teacher(g, m, v, k, kind):
