@@ -503,7 +503,7 @@ cudaError_t backward_t(int dt, const int32_t* tokens, long n, const T* dy, long 
     const Left left{(float*)(ws + sp.part), (int*)(ws + sp.head), counts, counts + 1, (int2*)(counts + 2)};
     const int gs = log2_up((32 + C - 1) / C);                    // a group: 128 bytes of the table at least
     const long groups = ((vocab - 1) >> gs) + 1, rows = ((groups + OWNERS - 1) >> OWNER_BITS) << gs;      // rows of an owner, the last of which may be behind the table
-    const int key_bits = std::max(1, log2_up(rows)), passes = (key_bits + MAX_BITS - 1) / MAX_BITS, bits = (key_bits + passes - 1) / passes;
+    const int key_bits = log2_up(rows), passes = (key_bits + MAX_BITS - 1) / MAX_BITS, bits = passes ? (key_bits + passes - 1) / passes : 0;      // (none: an owner has one row)
     static OncePerDevice once;
     cudaError_t e = allow_smem(once, (const void*)embed_sort_k, SORT_WARPS * (1 << MAX_BITS) * (int)sizeof(unsigned));
     if (e != cudaSuccess) return e;
