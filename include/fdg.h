@@ -374,7 +374,7 @@ FDG_API fdg_status fdg_recurrence_backward(const fdg_recurrence* shape, const vo
  *   logits  : logits_dtype, rows of `vocab`, logits_stride apart
  *   labels  : int32 [rows]; a label outside 0..vocab-1 takes its row out (loss and gradient zero).  NULL (weight 1 only): every row counts
  *   ids, teacher : int32, fp32 [rows][top]; an entry whose id is outside the vocabulary is left out, as is one of logit -infinity; entries with the same
- *             id count one by one; a row without an entry has no distillation term.  Not read when weight is 0 (may be NULL)
+ *             id count one by one; a row without an entry has no distillation term (with weight 1: loss and gradient zero, whatever its logits).  Not read when weight is 0 (may be NULL)
  *   loss    : fp32 [rows]
  *   dlogits : dlogits_dtype, or NULL for the loss alone; may be `logits` itself (same type and stride)
  * Types: logits and dlogits of the same type, or fp32 logits and bf16 dlogits.  vocab <= 262144, top <= 1024, 1e-6 <= temperature <= 1e6, 0 <= weight <= 1. */

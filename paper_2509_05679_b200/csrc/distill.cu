@@ -135,6 +135,10 @@ __global__ void __launch_bounds__(THREADS) distill_warp_k(DistillArgs a) {
     if (!g) return;
     t.ct = taught ? a.weight * a.tau : 0.f; t.it = 1.f / zt; t.i1 = HARD ? 1.f / z1 : 0.f;
     __syncwarp();                                   // what the loss needs of the row has been read (g may be x)
+    if (!HARD && !taught) {                         // neither term: zeros, whatever the logits are (0 times a sum of NaN would be NaN)
+        for (int v = lane; v < V; v += 32) st(g + v, 0.f);
+        return;
+    }
     for (int v = lane; v < V; v += 32) { float et, e1; exps(ld(x + v) - t.m, et, e1); st(g + v, t.at(et, e1, 0.f, HARD && v == label)); }
     if (!taught) return;
     __syncwarp();
@@ -357,7 +361,8 @@ __global__ void __launch_bounds__(THREADS, 3) distill_row_k(DistillArgs a, int r
         if (!CLUSTER && threadIdx.x == 0) a.loss[row] = loss;
         // the gradient without label and entries; the next row takes the place of this one
         const char* from = more ? chunk_of(next, threadIdx.x) : nullptr;
-        if (g && counts) {
+        const bool any = counts && (HARD || taught);         // a row with neither term has zeros, whatever its logits are (0 times a sum of NaN would be NaN)
+        if (g && any) {
             const float A = t.scale * t.ct * t.it, B = t.scale * t.c1 * t.i1;
             const float2 minus = make_float2(-t.m, -t.m), A2 = make_float2(A, A), B2 = make_float2(B, B);
             const bool vec = (uintptr_t)(g - q.phase) % (E * sizeof(TO)) == 0;   // the chunks of g start where those of x do
@@ -385,13 +390,13 @@ __global__ void __launch_bounds__(THREADS, 3) distill_row_k(DistillArgs a, int r
             }
         } else {
             for (int c = threadIdx.x; c < next.n; c += THREADS, from += THREADS * 16) fetch(next, c, from);
-            if (g)                                  // the row does not count
+            if (g)
                 for (int v = max(0, first * E - q.phase) + threadIdx.x; v < min(V, (first + n) * E - q.phase); v += THREADS) st(g + v, 0.f);
         }
         if (more) fetch_entries(row + step, buf ^ 1);
         asm volatile("cp.async.commit_group;" ::: "memory");
         // those, over it
-        if (g && counts) {
+        if (g && any) {
             const long base = (long)first * E - q.phase;
             auto fix = [&](int at, float s, float p) { float et, e1; exps(s - t.m, et, e1); st(g + base + at, t.at(et, e1, p, HARD && at == hit)); };
             __syncthreads();
