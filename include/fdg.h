@@ -324,7 +324,9 @@ FDG_API const char* fdg_static_last_error(void);
  *   - A call only enqueues kernels on `stream` (a cudaStream_t, NULL: the default stream): no allocation, no synchronisation, nothing kept between
  *     calls, so it may be captured into a CUDA graph, and calls on different streams, with workspaces of their own, may overlap.
  *   - Arithmetic and sums are in 32 bits, results are rounded once; equal inputs on equally aligned addresses of equal devices give equal bits.
- *   - Kernels that wait for copies of their own give up after about two seconds; outputs from there on are NaN.
+ *   - Kernels that wait (a recurrence's, for copies of its own and for the CTAs that share a sequence) give up after about two seconds: outputs from there on are NaN, and
+ *     inside fdg_step FDG_ERR_TIMEOUT is reported.  The environment variable FDG_WAIT_CYCLES, read once, sets other limits in cycles of an SM, "copies" or
+ *     "copies,peers"; 0 gives up at once, with which a caller can test what it does then.
  *   - A refused call launches nothing; fdg_op_last_error() says why (per thread). */
 
 /* Embedding lookup (the first layer of a token model): out[i] = scale * table[tokens[i]] for i < n.

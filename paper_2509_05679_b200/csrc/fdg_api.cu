@@ -177,9 +177,9 @@ struct fdg_ctx {
     char* dlogits;
     LossRecord* loss_ring;         // pinned host memory, 64 records
     int64_t* tags;
-    int* tc_err;                   // device word: set by a tensor-core kernel whose bounded wait gave up
+    int* tc_err;                   // device word: set by a kernel whose bounded wait gave up (tensor cores, batch-norm clusters, recurrences)
     bool mask_lost;                // during a module's backward pass: a launch that had to apply a ReLU mask was refused (the kernels that could replace it do not apply it)
-    bool any_tc;
+    bool waits;                    // has kernels with bounded waits
     bool graphs;                   // steady-state iterations run as graphs (off once recording one has failed)
     cudaEvent_t ingested;
     cudaStream_t cap;              // captures are recorded on it
@@ -737,7 +737,7 @@ RecurArgs recur_args(const fdg_ctx* c, const Op& o, const TensorDesc& ti, const 
     a.z = P.tensor(o.in); a.v = P.tensor(o.in) + (size_t)to.c * c->esz;
     a.z_t = a.v_t = ti.c; a.z_b = a.v_b = a.T * ti.c;
     a.y = P.tensor(o.out); a.y_t = to.c; a.y_b = a.T * to.c;
-    a.saved = P.stats(o);
+    a.saved = P.stats(o); a.err = c->tc_err;
     return a;
 }
 
@@ -1126,7 +1126,7 @@ bool build_tc_plans(fdg_ctx* c) {
                 o.fo.resize(o.y_ptrs.size());
                 for (size_t i = 0; i < o.y_ptrs.size(); ++i) ok = ok && tc::make_map_out(&o.fo[i], o.y_ptrs[i], g.Co, g.Wo, g.Ho, g.N, wt, ht);
                 if (!ok || o.dy_ptrs.empty() || o.y_ptrs.empty()) { o.stem_tc = false; o.stat_chunks = 0; continue; }
-                c->any_tc = true;
+                c->waits = true;
                 continue;
             }
             if (o.type != OP_CONV || !o.tc) continue;
@@ -1237,7 +1237,7 @@ bool build_tc_plans(fdg_ctx* c) {
             o.kf.sms = o.kd.sms = c->grid_sms;
             o.split_f = tc::small_split(o.kf); o.split_d = tc::small_split(o.kd);
             if (!ok) return false;
-            c->any_tc = true;
+            c->waits = true;
         }
     }
     return true;
@@ -1264,7 +1264,7 @@ fdg_status reset_state(fdg_ctx* ctx) {
 
 // Reads the device error word (the caller has synchronised the stream it cares about).
 fdg_status check_device_error(fdg_ctx* ctx) {
-    if (!ctx->any_tc && ctx->dt != 1) return FDG_OK;
+    if (!ctx->waits && ctx->dt != 1) return FDG_OK;
     int e = 0;
     CK(cudaMemcpy(&e, ctx->tc_err, sizeof(int), cudaMemcpyDeviceToHost));
     if (e) return fail(ctx, FDG_ERR_TIMEOUT, "a kernel gave up waiting on an mbarrier (code %d)", e);
@@ -1746,7 +1746,8 @@ fdg_status fdg_create(const fdg_layer* layers, int32_t n_layers, const int32_t* 
         std::vector<float> pf(ctx->P.begin(), ctx->P.end());
         if (cudaMemcpy(ctx->P_dev, pf.data(), pf.size() * sizeof(float), cudaMemcpyHostToDevice) != cudaSuccess) return bail(FDG_ERR_CUDA, "cudaMemcpy failed");
     }
-    ctx->any_tc = false;
+    ctx->waits = false;
+    for (const Module& m : ctx->mod) for (const Op& o : m.ops) ctx->waits |= o.type == OP_RECUR;
     if (!build_tc_plans(ctx)) return bail(FDG_ERR_CUDA, "cuTensorMapEncodeTiled rejected a tensor map");
     // a group must hold whole image tiles of every tensor-core tiling: a ragged tile would reach into the next group's rows
     for (Module& m : ctx->mod) {

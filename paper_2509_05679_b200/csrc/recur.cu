@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <type_traits>
 
 namespace fdg {
@@ -92,6 +93,8 @@ __device__ __forceinline__ bool try_wait(const uint64_t* bar, unsigned parity) {
     return ok;
 }
 constexpr long long WAIT_CYCLES = 4000000000ll;      // about 2 s
+constexpr long long STAY_CYCLES = 4000000ll;         // about 2 ms
+constexpr int TIMEOUT_CODE = 30;                     // in the caller's error word
 // The maps of gate, value and dy; used by the kernels whose rows lie on 16 bytes.
 struct Maps { tc::TensorMap t[3]; };
 
@@ -105,7 +108,8 @@ template <typename T, int ACC, int CX, int S, int TENSORS> struct Ring {
     static constexpr int BOX = G::TILE < 256 ? G::TILE : 256;      // rows of a tensor copy
     char* base;                                      // on 128 bytes
     uint64_t* full;                                  // [STAGES]
-    bool gave_up = false;
+    int lost = -1;                                   // >= 0: a wait of this thread gave up, when that many tiles had been asked for.  It asks for no more (a barrier takes
+                                                     // no arrival before its last phase is over), waits for nothing, and NaN takes the place of what it did not see.
     __device__ __forceinline__ char* mine(int stage, int tensor, int i) const {
         return base + stage * STAGE + tensor * TENSOR + (threadIdx.x / CX * S + i) * ROW + threadIdx.x % CX * (int)sizeof(V);
     }
@@ -122,7 +126,7 @@ template <typename T, int ACC, int CX, int S, int TENSORS> struct Ring {
     // rows t .. t + TILE - 1 of sequence b, channels c0 ..; g: this thread's first row and channel of every tensor, `left` of its channels exist, n of its rows count
     __device__ __forceinline__ void fetch(int stage, const Maps& maps, long c0, int t, long b, const T* const (&g)[TENSORS], const long (&step)[TENSORS], int left, int n) const {
         if constexpr (TMA) {
-            if (threadIdx.x != 0) return;
+            if (threadIdx.x != 0 || lost >= 0) return;
             const unsigned bar = smem_u32(full + stage);
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((unsigned)STAGE) : "memory");
 #pragma unroll
@@ -146,21 +150,26 @@ template <typename T, int ACC, int CX, int S, int TENSORS> struct Ring {
         }
     }
     __device__ __forceinline__ void issued() const { if constexpr (!TMA) asm volatile("cp.async.commit_group;" ::: "memory"); }
-    // the round's tile; LEFT: copies issued later that may be under way.  Bounded: a wait that gives up says so, and no other waits.
-    template <int LEFT> __device__ __forceinline__ void arrived(int stage, int round) {
+    // the round's tile; LEFT: copies issued later that may be under way.  Bounded by `limit` cycles (0: given up without a look).
+    template <int LEFT> __device__ __forceinline__ void arrived(int stage, int round, long long limit) {
         if constexpr (TMA) {
             const unsigned parity = (unsigned)(round / STAGES & 1);
-            if (gave_up || try_wait(full + stage, parity)) return;
+            if (lost >= 0 || (limit > 0 && try_wait(full + stage, parity))) return;
             const long long t0 = clock64();
-            while (!try_wait(full + stage, parity)) if (clock64() - t0 > WAIT_CYCLES) { gave_up = true; return; }
+            do {
+                if (clock64() - t0 >= limit) { lost = round + LEFT + 1; return; }
+            } while (!try_wait(full + stage, parity));
         } else copies_arrived<LEFT>();
     }
-    // in front of the end: what a wait that gave up left under way
-    __device__ __forceinline__ void drain(int rounds) const {
+    // in front of the end: what a wait that gave up left under way (bounded as well), and word of it
+    __device__ __forceinline__ void drain(int rounds, int* err) const {
+        if (lost < 0) return;
+        if (err) atomicCAS(err, 0, TIMEOUT_CODE);
         if constexpr (TMA) {
-            if (!gave_up) return;
+            if (threadIdx.x != 0) return;
+            const int n = min(rounds, lost);
             const long long t0 = clock64();
-            for (int r = max(0, rounds - STAGES); r < rounds; ++r) while (!try_wait(full + r % STAGES, (unsigned)(r / STAGES & 1))) if (clock64() - t0 > WAIT_CYCLES) return;
+            for (int r = max(0, n - STAGES); r < n; ++r) while (!try_wait(full + r % STAGES, (unsigned)(r / STAGES & 1))) if (clock64() - t0 > WAIT_CYCLES) return;
         }
     }
 };
@@ -215,15 +224,25 @@ template <int CH> struct Peers {
             asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(t), "f"(a), "f"(h), "r"(b) : "memory");
         }
     }
-    __device__ __forceinline__ bool arrived(int round) const {
+    // false: not within `limit` cycles (0: without a look)
+    __device__ __forceinline__ bool arrived(int round, long long limit) const {
         const unsigned bar = smem_u32(j->bar + (round & 1)), parity = (unsigned)(round >> 1 & 1);
         const long long t0 = clock64();
-        for (;;) {
+        while (limit > 0) {
             unsigned ok;
             asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
             if (ok) return true;
-            if (clock64() - t0 > WAIT_CYCLES) return false;
+            if (clock64() - t0 >= limit) break;
         }
+        return false;
+    }
+    // in front of the end.  Nobody leaves while others may write to its shared memory; a thread that gave up does not know of all the maps sent to its CTA, which take
+    // a microsecond or so, and stays a good while longer.
+    __device__ __forceinline__ void leave(bool gave_up) const {
+        cg::this_cluster().sync();
+        if (!gave_up) return;
+        const long long t0 = clock64();
+        while (clock64() - t0 < STAY_CYCLES) {}
     }
 };
 
@@ -236,6 +255,10 @@ template <int CX> struct Lane {
     static __device__ __forceinline__ int sub() { return ONE ? (threadIdx.x & 31) / CH : 0; }
     static __device__ __forceinline__ bool writes() { return ONE ? (threadIdx.x & 31) < CH : true; }
     float v[M];
+    __device__ __forceinline__ void fill(float x) {
+#pragma unroll
+        for (int j = 0; j < M; ++j) v[j] = x;
+    }
     __device__ __forceinline__ void set(const float* p) {
         if constexpr (ONE) v[0] = *p;
         else { const float4 r = *(const float4*)p; v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
@@ -338,7 +361,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
     for (int round = 0; round < rounds; ++round) {
         const int now = round & 1;
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);     // where the tile before was: it has been read
-        ring.template arrived<Rg::STAGES - 1>(stage, round);
+        ring.template arrived<Rg::STAGES - 1>(stage, round, p.wait_copies);
         // the map of this thread's steps
         const int n = steps_before<S>(len, t0);
         Four a[S], u[S], A, H;
@@ -358,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
             }
         };
         if (n == S) look(std::true_type()); else look(std::false_type());
-        if (ring.gave_up) u[0] = H = {both(NAN), both(NAN)};
+        if (ring.lost >= 0) u[0] = H = {both(NAN), both(NAN)};
         Chain<CX, true> chain;
         if constexpr (Lane<CX>::ONE) {
             __syncwarp();
@@ -370,17 +393,18 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
         __syncthreads();
         Lane<CX> in;
         if (CLUSTER) {                                             // the CTA's map goes to every CTA of the cluster
-            if (threadIdx.x < G::CH) {
+            if (threadIdx.x < G::CH && ring.lost < 0) {
                 float ta = 1.f, th = 0.f;
 #pragma unroll
                 for (int w = 0; w < G::TEAMS; ++w) { const float2 m = tot[now][w][threadIdx.x]; th = fmaf(m.x, th, m.y); ta *= m.x; }
                 peers.send(round, rank, R, ta, th);
             }
-            if (!ring.gave_up && !peers.arrived(round)) ring.gave_up = true;
+            if (ring.lost < 0 && !peers.arrived(round, p.wait_peers)) ring.lost = round + Rg::STAGES;
             for (int r = 0; r < R; ++r) {
                 if (r == rank) in = carry;
                 carry.through(&joined.at[now][r][first]);
             }
+            if (ring.lost >= 0) { in.fill(NAN); carry.fill(NAN); }        // what stands there is nobody's, or an earlier round's
         } else in.set(&carried[now][first]);
         for (int w = 0; w < team; ++w) in.through(&tot[now][w][first]);
         if (p.saved && team % (G::TEAMS / PARTS) == 0 && Lane<CX>::writes()) {
@@ -413,8 +437,8 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
         t0 += stride; y += y_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    ring.drain(rounds);
-    if (CLUSTER) cg::this_cluster().sync();                        // nobody leaves while others may write to its shared memory
+    ring.drain(rounds, p.err);
+    if (CLUSTER) peers.leave(ring.lost >= 0);
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
     if (p.state_out && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.state_out + b * p.C, c0, p.C);
 }
@@ -469,7 +493,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         const int now = round & 1;
         Lane<CX> in_h, in_g;
         in_h.read(tile < tiles ? p.saved + ((long)b * tiles + tile) * p.C : nullptr, c0, p.C);
-        ring.template arrived<Rg::STAGES - 2>(stage, round);
+        ring.template arrived<Rg::STAGES - 2>(stage, round, p.wait_copies);
         const int n = steps_before<STEPS>(len, t0);
         Four a[STEPS], q[STEPS], A, H, Q;
         auto look = [&](auto all) {
@@ -491,7 +515,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
             }
         };
         if (n == STEPS) look(std::true_type()); else look(std::false_type());
-        if (ring.gave_up) H = Q = {both(NAN), both(NAN)};
+        if (ring.lost >= 0) H = Q = {both(NAN), both(NAN)};
         float* own[3];
 #pragma unroll
         for (int k = 0; k < 3; ++k)
@@ -513,17 +537,18 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         __syncthreads();
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);     // where the tile before was: it has been read
         if (CLUSTER) {
-            if (threadIdx.x < G::CH) {
+            if (threadIdx.x < G::CH && ring.lost < 0) {
                 float ta = 1.f, tq = 0.f;
 #pragma unroll
                 for (int w = G::TEAMS - 1; w >= 0; --w) { const float2 m = tot_g[now][w][threadIdx.x]; tq = fmaf(m.x, tq, m.y); ta *= m.x; }
                 peers.send(round, rank, R, ta, tq);
             }
-            if (!ring.gave_up && !peers.arrived(round)) ring.gave_up = true;
+            if (ring.lost < 0 && !peers.arrived(round, p.wait_peers)) ring.lost = round + Rg::STAGES;
             for (int r = R - 1; r >= 0; --r) {
                 if (r == rank) in_g = carry;
                 carry.through(&joined.at[now][r][first]);
             }
+            if (ring.lost >= 0) { in_g.fill(NAN); carry.fill(NAN); }
         } else in_g.set(&carried[now][first]);
         for (int w = 0; w < team; ++w) in_h.through(&tot_h[now][w][first]);
         for (int w = G::TEAMS - 1; w > team; --w) in_g.through(&tot_g[now][w][first]);
@@ -538,6 +563,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
             before[0] = {make_float2(in_h.v[0], in_h.v[1]), make_float2(in_h.v[2], in_h.v[3])};
             g = {make_float2(in_g.v[0], in_g.v[1]), make_float2(in_g.v[2], in_g.v[3])};
         }
+        if (ring.lost >= 0) before[0] = g = {both(NAN), both(NAN)};       // the maps say it to the others, this to the thread's own steps
 #pragma unroll
         for (int i = 0; i + 1 < STEPS; ++i) {
             const Four v = ring.get(stage, 1, i);
@@ -579,8 +605,8 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         t0 -= stride; tile -= R; dz -= dz_round; dv -= dv_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    ring.drain(rounds);
-    if (CLUSTER) cg::this_cluster().sync();
+    ring.drain(rounds, p.err);
+    if (CLUSTER) peers.leave(ring.lost >= 0);
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
     if (p.dstate && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.dstate + b * p.C, c0, p.C);
 }
@@ -625,6 +651,24 @@ Cut cut(long B, long T, long C) {
     return best;
 }
 
+// How long the kernels' waits last: the environment's FDG_WAIT_CYCLES, "copies" or "copies,peers".
+struct Waits { long long copies, peers; };
+const Waits& waits() {
+    static const Waits known = [] {
+        Waits w{WAIT_CYCLES, WAIT_CYCLES};
+        if (const char* s = getenv("FDG_WAIT_CYCLES")) {
+            char* end;
+            const long long a = strtoll(s, &end, 10);
+            if (end != s && a >= 0) {
+                w = {a, a};
+                if (*end == ',') { const long long b = strtoll(end + 1, nullptr, 10); if (b >= 0) w.peers = b; }
+            }
+        }
+        return w;
+    }();
+    return known;
+}
+
 // false: the tensors cannot be described (they are too far apart)
 template <typename T, int CX, int S>
 bool make_maps(const RecurArgs& a, bool back, Maps& m) {
@@ -644,7 +688,9 @@ cudaError_t launch(const RecurArgs& a, int R, cudaStream_t s) {
     const cudaError_t e = allow_smem(once, (const void*)k, Rg::BYTES);
     if (e != cudaSuccess) return e;
     const int slices = (int)((a.C + Geo<CX, S>::CH - 1) / Geo<CX, S>::CH);
-    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, Rg::BYTES, s, CLUSTER ? R : 0, a, maps, R, slices);
+    RecurArgs p = a;
+    p.wait_copies = waits().copies; p.wait_peers = waits().peers;
+    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, Rg::BYTES, s, CLUSTER ? R : 0, p, maps, R, slices);
 }
 template <typename T, int ACC, bool BACK>
 cudaError_t pick(const RecurArgs& a, cudaStream_t s) {
