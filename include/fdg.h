@@ -345,6 +345,7 @@ FDG_API fdg_status fdg_embedding_backward(const int32_t* dev_tokens, int64_t n, 
 
 /* Gated linear recurrence along the steps of `batch` sequences, every channel by itself:
  *   a_t = sigmoid(gate_t),   h_t = a_t h_{t-1} + (1 - a_t) value_t,   y_t = h_t   (h_0 = state_in, or zero)
+ * (a_t is at least 2^-126, the least normal number: gates below -87.3, minus infinity among them, count as -87.3.)
  * A single step (steps = 1, state_in, state_out) serves one new token; state_out may be state_in.
  * Tensors are [batch][steps][channels] (steps <= 2^30, channels <= 2^20) with strides of their own between sequences and between steps, channels contiguous (so gate and value may be the
  * halves of one tensor, or time-major).  state_*, dstate_* are fp32 [batch][channels], contiguous; saved is written by the forward call and read by the

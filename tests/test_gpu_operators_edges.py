@@ -57,3 +57,36 @@ def test_a_row_without_an_entry_has_no_gradient_whatever_its_logits(ops, how, v,
     if types[0] == types[1]:
         ops.distill_loss(logits, None, ids, teacher, temperature=2.0, scale=0.5, out=logits)
         assert torch.equal(logits, out)
+
+
+# ---- recurrence: gates far below zero
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("steps", [1, 9])
+def test_gates_far_below_zero(ops, steps, dtype):
+    """sigmoid is held to its own size down to the least normal number, 2^-126 at gate -87.3, and stays there below: what a state and a gradient keep of it is a product with it.
+    One sequence a gate, values of zero, so that a state is the product of its gates' sigmoids and nothing else (only the first step's gate is far below zero: a second one would
+    underflow); dgate of that step is a (1 - a) dy (h_0 - 0)."""
+    gates = torch.cat([-torch.arange(60.0, 90.0, 0.25, device="cuda"), torch.tensor([-87.33, -87.34, -88.0, -100.0, -1000.0, -1e30, -INF], device="cuda")]).to(dtype)
+    b, c = len(gates), 24
+    gate = torch.zeros(b, steps, c, device="cuda", dtype=dtype)
+    gate[:, 0] = gates[:, None]
+    value = torch.zeros_like(gate)
+    g = _gen(5)
+    state, dstate = 1 + torch.rand(b, c, generator=g, device="cuda"), 1 + torch.rand(b, c, generator=g, device="cuda")
+    y, last, saved = ops.recurrence(gate, value, state=state, for_grad=True)
+    dgate, dvalue = torch.empty_like(gate), torch.empty_like(gate)
+    first = ops.recurrence_grad(gate, value, torch.zeros_like(gate), saved, dgate=dgate, dvalue=dvalue, dstate=dstate)
+    z = gates.double()
+    a = torch.sigmoid(z).clamp(min=2.0 ** -126)[:, None]
+    q = torch.sigmoid(-z)[:, None]
+    behind = 0.5 ** (steps - 1)                                # sigmoid(0) of the steps behind: exact, but for results below the least normal number
+    # the gate: (8 + |z|) U (operators_reference); products: 2 U a step; 2^-149 for what falls below the least normal number
+    rel = (8 + z.abs().clamp(max=87.4) + 2 * (steps + 3))[:, None] * ref.U
+    def near(got, want, what):
+        ref.check(got, want, ref.store(want, rel * want.abs() + 2.0 ** -149 * (steps + 3), got.dtype), what)
+    near(last, a * behind * state.double(), "state")
+    near(y[:, 0], a * state.double(), "y")
+    near(first, a * behind * dstate.double(), "gradient of the first state")
+    near(dgate[:, 0], a * q * behind * dstate.double() * state.double(), "dgate")
+    near(dvalue[:, 0], q * behind * dstate.double(), "dvalue")
