@@ -3,7 +3,8 @@ gated linear recurrence and its gradient, distillation loss with its gradient.
 
 Arguments are marshalled and checked here; the work is done by the library's kernels, on torch's current stream of the tensors' device.
 Outputs (unless given) and workspaces come from torch's caching allocator on that stream, so calls can be captured into a CUDA graph
-like torch's own.  There is no CPU path.  Nothing is recorded for autograd: the gradients are calls of their own.
+like torch's own.  There is no CPU path.  Nothing is recorded for autograd: the gradients are calls of their own, and a tensor that autograd follows
+(requires_grad, under grad mode) is refused; call under ``torch.no_grad()`` or pass ``t.detach()``.
 
 The host's share of a small call is most of its time, so a check that holds costs a comparison and no text is made for it.
 """
@@ -20,6 +21,7 @@ from .binding import FdgError
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1}
 _fn = {}
+_grad_mode = torch.is_grad_enabled
 
 
 def _refuse(what: str):
@@ -58,6 +60,8 @@ def _dense(name: str, t, dtype, shape, device) -> None:
     """t is a contiguous CUDA tensor of this type, shape (as far as given) and device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name} must be a CUDA tensor")
+    if t.requires_grad and _grad_mode():
+        _refuse(f"{name} requires a gradient, which nothing here records: call under torch.no_grad(), or pass {name}.detach()")
     if t.dtype is not dtype:
         _refuse(f"{name} must be of type {dtype}, not {t.dtype}")
     if device is not None and t.device != device:
@@ -73,6 +77,8 @@ def _rows(name: str, t, dtype, ndim: int, shape, device):
     stride in torch: it gets the one of a contiguous tensor."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name} must be a CUDA tensor")
+    if t.requires_grad and _grad_mode():
+        _refuse(f"{name} requires a gradient, which nothing here records: call under torch.no_grad(), or pass {name}.detach()")
     if t.dtype is not dtype and (dtype is not None or t.dtype not in _DTYPE):
         _refuse(f"{name} must be of type {dtype or 'float32 or bfloat16'}, not {t.dtype}")
     if device is not None and t.device != device:

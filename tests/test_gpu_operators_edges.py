@@ -90,3 +90,35 @@ def test_gates_far_below_zero(ops, steps, dtype):
     near(first, a * behind * dstate.double(), "gradient of the first state")
     near(dgate[:, 0], a * q * behind * dstate.double() * state.double(), "dgate")
     near(dvalue[:, 0], q * behind * dstate.double(), "dvalue")
+
+
+# ---- inputs that autograd follows
+
+def test_tensors_that_autograd_follows_are_refused(ops):
+    """A result without a history would lose the gradient without a word; where nothing is recorded (no_grad, a detached tensor) the call goes through."""
+    from paper_2509_05679_b200.binding import FdgError
+    tok = torch.zeros(4, dtype=torch.int32, device="cuda")
+    x = lambda *s: torch.zeros(*s, device="cuda")
+    p = lambda *s: torch.zeros(*s, device="cuda", requires_grad=True)
+    saved = ops.recurrence(x(2, 3, 4), x(2, 3, 4), for_grad=True)[2]
+    ids = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    calls = [
+        lambda f: ops.embedding(tok, f(5, 4)),
+        lambda f: ops.embedding(tok, x(5, 4), out=f(4, 4)),
+        lambda f: ops.embedding_grad(tok, f(4, 4), 5),
+        lambda f: ops.embedding_grad(tok, x(4, 4), 5, out=f(5, 4)),
+        lambda f: ops.recurrence(f(2, 3, 4), x(2, 3, 4)),
+        lambda f: ops.recurrence(x(2, 3, 4), f(2, 3, 8)[..., 4:]),
+        lambda f: ops.recurrence(x(2, 3, 4), x(2, 3, 4), state=f(2, 4)),
+        lambda f: ops.recurrence_grad(x(2, 3, 4), x(2, 3, 4), f(2, 3, 4), saved, dgate=x(2, 3, 4), dvalue=x(2, 3, 4)),
+        lambda f: ops.recurrence_grad(x(2, 3, 4), x(2, 3, 4), x(2, 3, 4), saved, dgate=x(2, 3, 4), dvalue=x(2, 3, 4), dstate=f(2, 4)),
+        lambda f: ops.distill_loss(f(2, 9), None, ids, x(2, 1)),
+        lambda f: ops.distill_loss(x(2, 9), None, ids, f(2, 1)),
+    ]
+    for n, call in enumerate(calls):
+        with pytest.raises(FdgError, match="no_grad"):
+            call(p)
+            pytest.fail(f"call {n} went through")
+        with torch.no_grad():
+            call(p)
+        call(lambda *s: p(*s).detach())
