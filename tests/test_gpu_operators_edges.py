@@ -122,3 +122,35 @@ def test_tensors_that_autograd_follows_are_refused(ops):
         with torch.no_grad():
             call(p)
         call(lambda *s: p(*s).detach())
+
+
+# ---- embedding gradient: sums that have to be exact
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("kind", ["uniform", "padded", "one", "skewed", "two"])
+@pytest.mark.parametrize("n,vocab,c", [(512, 40, 24), (513, 1, 5), (9000, 1000, 64), (20000, 3, 1032), (40000, 33000, 16), (70000, 300000, 8), (131072, 5, 256), (150001, 17, 40),
+                                       (300007, 32000, 3), (1000003, 700, 2)])
+def test_embedding_gradient_of_whole_numbers(ops, n, vocab, c, kind, dtype):
+    """Whole numbers up to 8: a sum of a million of them is exact in 32 bits in any order, so a row left out, taken twice or added to a wrong token shows, however many there are."""
+    g = _gen(n + c)
+    tok = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    if kind == "padded":
+        tok[torch.rand(n, generator=g, device="cuda") < 0.4] = -1
+        tok[n // 2] = vocab
+    elif kind == "one":
+        tok[:] = vocab // 2
+    elif kind == "two":                                     # runs of one token that end inside a tile, over many tiles
+        tok[:] = 0
+        tok[n // 3:] = vocab - 1
+    elif kind == "skewed":
+        tok = ((torch.rand(n, generator=g, device="cuda").clamp(min=1e-6).log2() * -0.5).floor().int()) % vocab
+    dy = torch.randint(-8, 9, (n, c), generator=g, device="cuda", dtype=torch.int32)
+    keep = (tok >= 0) & (tok < vocab)
+    want = torch.zeros(vocab, c, dtype=torch.int64, device="cuda").index_add_(0, tok[keep].long(), dy[keep].long())
+    rows = dy.to(dtype)
+    rows[~keep] = NAN
+    dw = ops.embedding_grad(tok, rows, vocab)
+    assert torch.equal(dw, want.float())
+    start = torch.randint(-1000, 1000, (vocab, c), generator=g, device="cuda", dtype=torch.int32)
+    dw = ops.embedding_grad(tok, rows, vocab, scale=0.5, out=start.float(), accumulate=True)
+    assert torch.equal(dw, (start + want.double() * 0.5).float())
