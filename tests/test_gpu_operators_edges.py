@@ -154,3 +154,84 @@ def test_embedding_gradient_of_whole_numbers(ops, n, vocab, c, kind, dtype):
     start = torch.randint(-1000, 1000, (vocab, c), generator=g, device="cuda", dtype=torch.int32)
     dw = ops.embedding_grad(tok, rows, vocab, scale=0.5, out=start.float(), accumulate=True)
     assert torch.equal(dw, (start + want.double() * 0.5).float())
+
+
+# ---- calls that differ from one another in layout, and replays on other data
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_broadcast_rows_and_odd_addresses(ops, dtype):
+    """One gradient row and one row of logits for all (strides of zero), ids and results on the address after the first: as the dense calls."""
+    g = _gen(11)
+    for n, vocab, c in [(300, 50, 40), (3001, 700, 64), (3001, 700, 33)]:
+        tok = torch.randint(-1, vocab, (n + 1,), generator=g, device="cuda", dtype=torch.int32)[1:]
+        row = torch.randint(-8, 9, (1, c), generator=g, device="cuda").to(dtype)
+        want = torch.zeros(vocab, c, device="cuda", dtype=torch.int64).index_add_(0, tok[tok >= 0].long(), row.long().expand(int((tok >= 0).sum()), c))
+        out = torch.full((vocab * c + 1,), NAN, device="cuda")[1:].view(vocab, c)
+        assert torch.equal(ops.embedding_grad(tok, row.expand(n, c), vocab, out=out), want.float())
+        table = _normal(g, vocab, c, dtype=dtype)
+        assert torch.equal(ops.embedding(tok, table), torch.where((tok >= 0)[:, None], table[tok.clamp(min=0).long()], 0.0))
+    for v in (70, 6001, 70001):
+        m, k = 5, 6
+        row, teacher = _normal(g, 1, v, dtype=dtype), _normal(g, m, k)
+        ids = torch.randint(0, v, (m, k), generator=g, device="cuda", dtype=torch.int32)
+        labels = torch.randint(0, v, (m,), generator=g, device="cuda", dtype=torch.int32)
+        a = ops.distill_loss(row.expand(m, v), labels, ids, teacher, temperature=1.5, weight=0.5)
+        b = ops.distill_loss(row.expand(m, v).contiguous(), labels, ids, teacher, temperature=1.5, weight=0.5)
+        (el, bl), (eg, bg) = ref.distill(row.expand(m, v), labels, ids, teacher, 1.5, 0.5, 1.0, dtype)
+        for loss, grad in (a, b):
+            ref.check(loss, el, bl, "loss")
+            ref.check(grad, eg, bg, "gradient")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("b,n,c", [(1, 1, 8), (3, 1, 20), (1, 900, 24), (6, 130, 40), (2, 2500, 17)])
+def test_a_recurrence_whose_tensors_lie_differently(ops, b, n, c, dtype):
+    """Gates time-major, values inside a wider tensor, dy one row for all steps, results in layouts of their own: as with dense tensors, bit by bit."""
+    g = _gen(b + n + c)
+    gate, value, row = _normal(g, b, n, c, dtype=dtype), _normal(g, b, n, c, dtype=dtype), _normal(g, b, 1, c, dtype=dtype)
+    state, dstate = _normal(g, b, c), _normal(g, b, c)
+    tm = lambda t: torch.empty(n, b, c, dtype=dtype, device="cuda").transpose(0, 1).copy_(t)
+    wide = lambda t: torch.full((b, n, 3 * c + 2), NAN, dtype=dtype, device="cuda")[..., c + 1:2 * c + 1].copy_(t)
+    runs = []
+    for ga, va, dy, y, dz, dv in [(gate, value, row.expand(b, n, c).contiguous(), None, torch.empty_like(gate), torch.empty_like(gate)),
+                                  (tm(gate), wide(value), row.expand(b, n, c), wide(gate), wide(gate), tm(gate))]:
+        y, last, saved = ops.recurrence(ga, va, state=state, for_grad=True, out=y)
+        first = ops.recurrence_grad(ga, va, dy, saved, dgate=dz, dvalue=dv, dstate=dstate)
+        runs.append((y, last, first, dz, dv))
+    assert all(torch.equal(p, q) for p, q in zip(*runs))
+
+
+def test_a_captured_run_answers_for_the_data_it_is_replayed_on(ops):
+    """Captured once; the data of every replay are others: ids with other repetitions, lengths, lists of the teacher, labels."""
+    g = _gen(21)
+    b, n, c, vocab, k = 3, 700, 40, 300, 5
+    tok = torch.zeros(b * n, dtype=torch.int32, device="cuda")
+    x, dy, state = torch.zeros(b, n, 2 * c, device="cuda", dtype=BF16), torch.zeros(b, n, c, device="cuda", dtype=BF16), torch.zeros(b, c, device="cuda")
+    lengths = torch.full((b,), n, dtype=torch.int32, device="cuda")
+    logits, labels = torch.zeros(b * n, vocab, device="cuda"), torch.zeros(b * n, dtype=torch.int32, device="cuda")
+    ids, teacher = torch.zeros(b * n, k, dtype=torch.int32, device="cuda"), torch.zeros(b * n, k, device="cuda")
+    wide, wids, wteacher = torch.zeros(4, 70000, device="cuda"), torch.zeros(4, k, dtype=torch.int32, device="cuda"), torch.zeros(4, k, device="cuda")
+
+    def run():
+        y, last, saved = ops.recurrence(x[..., :c], x[..., c:], state=state, lengths=lengths, for_grad=True)
+        dx = torch.empty_like(x)
+        first = ops.recurrence_grad(x[..., :c], x[..., c:], dy, saved, dgate=dx[..., :c], dvalue=dx[..., c:], dstate=state, lengths=lengths)
+        return [y, last, dx, first, ops.embedding_grad(tok, dy.view(b * n, c), vocab), *ops.distill_loss(logits, labels, ids, teacher, temperature=2.0, weight=0.5),
+                *ops.distill_loss(wide, None, wids, wteacher, temperature=2.0)]
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for i in range(4):
+        tok.copy_(torch.randint(-1, vocab >> (3 * i) or 1, (b * n,), generator=g, device="cuda"))
+        for t in (x, dy, state, logits, teacher, wide, wteacher):
+            t.copy_(_normal(g, *t.shape))
+        lengths.copy_(torch.randint(0, n + 1, (b,), generator=g, device="cuda"))
+        labels.copy_(torch.randint(-1, vocab, (b * n,), generator=g, device="cuda"))
+        for t, v in ((ids, vocab), (wids, 70000)):
+            t.copy_(torch.randint(-1, v if i % 2 else 3, t.shape, generator=g, device="cuda"))       # (every other time: entries with the same id)
+        for t in got:
+            t.fill_(NAN)
+        graph.replay()
+        assert all(torch.equal(p, q) for p, q in zip(got, run()))
