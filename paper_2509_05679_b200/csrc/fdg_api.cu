@@ -737,7 +737,7 @@ RecurArgs recur_args(const fdg_ctx* c, const Op& o, const TensorDesc& ti, const 
     a.z = P.tensor(o.in); a.v = P.tensor(o.in) + (size_t)to.c * c->esz;
     a.z_t = a.v_t = ti.c; a.z_b = a.v_b = a.T * ti.c;
     a.y = P.tensor(o.out); a.y_t = to.c; a.y_b = a.T * to.c;
-    a.saved = P.stats(o); a.err = c->tc_err;
+    a.saved = P.stats(o);
     return a;
 }
 
@@ -826,7 +826,7 @@ void forward_ops(fdg_ctx* c, int kk, int64_t batch, int64_t version, int group, 
             case OP_EMBED:
                 embed_forward(dt, (const int32_t*)T(o.in), (long)wn.n * ti.h * ti.w, wbig(c, m, version, o.w_off, rep), o.g.C, o.g.Co, o.scale, T(o.out), o.g.Co, s);
                 break;
-            case OP_RECUR: recur_forward(dt, recur_args(c, o, ti, to, P), s); break;
+            case OP_RECUR: recur_forward(dt, recur_args(c, o, ti, to, P), c->tc_err, s); break;
         }
     }
 }
@@ -875,7 +875,7 @@ bool forward_op_replicas(fdg_ctx* c, int kk, int64_t batch, int64_t version, siz
         case OP_GAP: gap_forward(dt, P.tensor(o.in), P.tensor(o.out), c->M, ti.h * ti.w, ti.c, s); return true;
         case OP_ADD: add_forward(dt, P.tensor(o.in), P.tensor(o.in2), P.tensor(o.out), to.elems() * c->M, s); return true;
         case OP_EMBED: return false;
-        case OP_RECUR: recur_forward(dt, recur_args(c, o, ti, to, P), s); return true;
+        case OP_RECUR: recur_forward(dt, recur_args(c, o, ti, to, P), c->tc_err, s); return true;
     }
     return false;
 }
@@ -913,7 +913,7 @@ void recur_back(fdg_ctx* c, const Op& o, const TensorDesc& ti, const TensorDesc&
     a.dz = gin; a.dv = gin + (size_t)to.c * c->esz;
     a.dz_t = a.dv_t = ti.c; a.dz_b = a.dv_b = a.T * ti.c;
     a.accum = o.acc_in;
-    recur_backward(c->dt, a, s);
+    recur_backward(c->dt, a, c->tc_err, s);
 }
 
 // The ops i1 - 1 down to i0 of a module's backward pass on one group's rows.

@@ -160,7 +160,7 @@ fdg_status fdg_recurrence_forward(const fdg_recurrence* s, const void* gate, con
     a.B = s->batch; a.T = s->steps; a.C = s->channels;
     a.z = gate; a.v = value; a.z_b = s->gate_batch; a.z_t = s->gate_step; a.v_b = s->value_batch; a.v_t = s->value_step;
     a.lengths = lengths; a.state = state_in; a.y = y; a.y_b = s->y_batch; a.y_t = s->y_step; a.state_out = state_out; a.saved = (float*)saved;
-    return enqueued(fn, recur_forward(s->dtype, a, (cudaStream_t)stream));
+    return enqueued(fn, recur_forward(s->dtype, a, nullptr, (cudaStream_t)stream));
 }
 
 fdg_status fdg_recurrence_backward(const fdg_recurrence* s, const void* gate, const void* value, const int32_t* lengths, const void* saved, const void* dy,
@@ -192,7 +192,7 @@ fdg_status fdg_recurrence_backward(const fdg_recurrence* s, const void* gate, co
     a.lengths = lengths; a.saved = (float*)saved;
     a.dy = dy; a.dy_b = s->dy_batch; a.dy_t = s->dy_step; a.dstate_out = dstate_out;
     a.dz = dgate; a.dz_b = s->dgate_batch; a.dz_t = s->dgate_step; a.dv = dvalue; a.dv_b = s->dvalue_batch; a.dv_t = s->dvalue_step; a.dstate = dstate_in;
-    return enqueued(fn, recur_backward(s->dtype, a, (cudaStream_t)stream));
+    return enqueued(fn, recur_backward(s->dtype, a, nullptr, (cudaStream_t)stream));
 }
 
 fdg_status fdg_distill_loss(const fdg_distill* d, const void* logits, const int32_t* labels, const int32_t* ids, const float* teacher, float* loss, void* dlogits,

@@ -96,6 +96,8 @@ __device__ __forceinline__ bool try_wait(const uint64_t* bar, unsigned parity) {
 constexpr long long WAIT_CYCLES = 4000000000ll;      // about 2 s
 constexpr long long STAY_CYCLES = 4000000ll;         // about 2 ms
 constexpr int TIMEOUT_CODE = 30;                     // in the caller's error word
+// How long waits last, in cycles; the caller's error word.  (Not in RecurArgs: with 24 bytes more of arguments a launch takes the host 0.7 us longer, a fifth of a single step's call.)
+struct Waits { long long copies, peers; int* err; };
 // The maps of gate, value and dy; used by the kernels whose rows lie on 16 bytes.
 struct Maps { tc::TensorMap t[3]; };
 
@@ -318,7 +320,7 @@ __device__ __forceinline__ void store(float2* p, const Four& A, const Four& H) {
 // One barrier a tile: behind it a warp goes through the maps of the teams in front of it by itself, and the last steps' threads leave the state for the
 // next tile, which the next tile's barrier orders.  What stands there is kept twice, by the round's parity.
 template <typename T, int ACC, int CX, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __grid_constant__ Maps maps, int ranks, int slices) {
+__global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __grid_constant__ Maps maps, Waits waits, int ranks, int slices) {
     const int R = CLUSTER ? ranks : 1;
     constexpr int S = STEPS_FWD<T>, PARTS = S / STEPS;         // tiles of the backward pass in one of this
     using G = Geo<CX, S>;
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
     for (int round = 0; round < rounds; ++round) {
         const int now = round & 1;
         fetch_tile(stage == 0 ? Rg::STAGES - 1 : stage - 1);     // where the tile before was: it has been read
-        ring.template arrived<Rg::STAGES - 1>(stage, round, p.wait_copies);
+        ring.template arrived<Rg::STAGES - 1>(stage, round, waits.copies);
         // the map of this thread's steps
         const int n = steps_before<S>(len, t0);
         Four a[S], u[S], A, H;
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
                 for (int w = 0; w < G::TEAMS; ++w) { const float2 m = tot[now][w][threadIdx.x]; th = fmaf(m.x, th, m.y); ta *= m.x; }
                 peers.send(round, rank, R, ta, th);
             }
-            if (ring.lost < 0 && !peers.arrived(round, p.wait_peers)) ring.lost = round + Rg::STAGES;
+            if (ring.lost < 0 && !peers.arrived(round, waits.peers)) ring.lost = round + Rg::STAGES;
             for (int r = 0; r < R; ++r) {
                 if (r == rank) in = carry;
                 carry.through(&joined.at[now][r][first]);
@@ -438,14 +440,14 @@ __global__ void __launch_bounds__(THREADS, 2) recur_fwd_k(RecurArgs p, const __g
         t0 += stride; y += y_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    ring.drain(rounds, p.err);
+    ring.drain(rounds, waits.err);
     if (CLUSTER) peers.leave(ring.lost >= 0);
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
     if (p.state_out && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.state_out + b * p.C, c0, p.C);
 }
 
 template <typename T, int ACC, int CX, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __grid_constant__ Maps maps, int ranks, int slices) {
+__global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __grid_constant__ Maps maps, Waits waits, int ranks, int slices) {
     const int R = CLUSTER ? ranks : 1;
     using G = Geo<CX, STEPS>;
     using Rg = Ring<T, ACC, CX, STEPS, 3>;
@@ -494,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         const int now = round & 1;
         Lane<CX> in_h, in_g;
         in_h.read(tile < tiles ? p.saved + ((long)b * tiles + tile) * p.C : nullptr, c0, p.C);
-        ring.template arrived<Rg::STAGES - 2>(stage, round, p.wait_copies);
+        ring.template arrived<Rg::STAGES - 2>(stage, round, waits.copies);
         const int n = steps_before<STEPS>(len, t0);
         Four a[STEPS], q[STEPS], A, H, Q;
         auto look = [&](auto all) {
@@ -544,7 +546,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
                 for (int w = G::TEAMS - 1; w >= 0; --w) { const float2 m = tot_g[now][w][threadIdx.x]; tq = fmaf(m.x, tq, m.y); ta *= m.x; }
                 peers.send(round, rank, R, ta, tq);
             }
-            if (ring.lost < 0 && !peers.arrived(round, p.wait_peers)) ring.lost = round + Rg::STAGES;
+            if (ring.lost < 0 && !peers.arrived(round, waits.peers)) ring.lost = round + Rg::STAGES;
             for (int r = R - 1; r >= 0; --r) {
                 if (r == rank) in_g = carry;
                 carry.through(&joined.at[now][r][first]);
@@ -606,7 +608,7 @@ __global__ void __launch_bounds__(THREADS, 2) recur_bwd_k(RecurArgs p, const __g
         t0 -= stride; tile -= R; dz -= dz_round; dv -= dv_round;
         stage = stage + 1 == Rg::STAGES ? 0 : stage + 1;
     }
-    ring.drain(rounds, p.err);
+    ring.drain(rounds, waits.err);
     if (CLUSTER) peers.leave(ring.lost >= 0);
     else { __syncthreads(); carry.set(&carried[rounds & 1][first]); }
     if (p.dstate && rank == 0 && threadIdx.x < G::TEAM && Lane<CX>::writes()) carry.write(p.dstate + b * p.C, c0, p.C);
@@ -652,22 +654,21 @@ Cut cut(long B, long T, long C) {
     return best;
 }
 
-// How long the kernels' waits last: the environment's FDG_WAIT_CYCLES, "copies" or "copies,peers".
-struct Waits { long long copies, peers; };
-const Waits& waits() {
+// The limits of the waits: two seconds or so, or the environment's FDG_WAIT_CYCLES, "copies" or "copies,peers".
+Waits limits(int* err) {
     static const Waits known = [] {
-        Waits w{WAIT_CYCLES, WAIT_CYCLES};
+        Waits w{WAIT_CYCLES, WAIT_CYCLES, nullptr};
         if (const char* s = getenv("FDG_WAIT_CYCLES")) {
             char* end;
             const long long a = strtoll(s, &end, 10);
             if (end != s && a >= 0) {
-                w = {a, a};
+                w.copies = w.peers = a;
                 if (*end == ',') { const long long b = strtoll(end + 1, nullptr, 10); if (b >= 0) w.peers = b; }
             }
         }
         return w;
     }();
-    return known;
+    return {known.copies, known.peers, err};
 }
 
 // false: the tensors cannot be described (they are too far apart)
@@ -679,39 +680,37 @@ bool make_maps(const RecurArgs& a, bool back, Maps& m) {
            (!back || tc::make_map_rows(&m.t[2], dt, a.dy, a.C, a.T, a.B, a.dy_t, a.dy_b, Geo<CX, S>::CH, box));
 }
 template <typename T, int ACC, int CX, bool BACK, bool CLUSTER>
-cudaError_t launch(const RecurArgs& a, int R, cudaStream_t s) {
+cudaError_t launch(const RecurArgs& a, int R, int* err, cudaStream_t s) {
     constexpr int S = BACK ? STEPS : STEPS_FWD<T>;
     using Rg = Ring<T, ACC, CX, S, BACK ? 3 : 2>;
     Maps maps{};
-    if constexpr (Rg::TMA) if (!make_maps<T, CX, S>(a, BACK, maps)) return launch<T, (sizeof(T) == 2 ? 2 : 1), CX, BACK, CLUSTER>(a, R, s);
+    if constexpr (Rg::TMA) if (!make_maps<T, CX, S>(a, BACK, maps)) return launch<T, (sizeof(T) == 2 ? 2 : 1), CX, BACK, CLUSTER>(a, R, err, s);
     static OncePerDevice once;
     const auto k = BACK ? recur_bwd_k<T, ACC, CX, CLUSTER> : recur_fwd_k<T, ACC, CX, CLUSTER>;
     const cudaError_t e = allow_smem(once, (const void*)k, Rg::BYTES);
     if (e != cudaSuccess) return e;
     const int slices = (int)((a.C + Geo<CX, S>::CH - 1) / Geo<CX, S>::CH);
-    RecurArgs p = a;
-    p.wait_copies = waits().copies; p.wait_peers = waits().peers;
-    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, Rg::BYTES, s, CLUSTER ? R : 0, p, maps, R, slices);
+    return klaunch_cluster(k, (unsigned)(a.B * slices * R), THREADS, Rg::BYTES, s, CLUSTER ? R : 0, a, maps, limits(err), R, slices);
 }
 template <typename T, int ACC, bool BACK>
-cudaError_t pick(const RecurArgs& a, cudaStream_t s) {
+cudaError_t pick(const RecurArgs& a, int* err, cudaStream_t s) {
     const Cut k = cut(a.B, a.T, a.C);
     switch (k.cx) {
-        case 4: return k.r > 1 ? launch<T, ACC, 4, BACK, true>(a, k.r, s) : launch<T, ACC, 4, BACK, false>(a, 1, s);
-        case 8: return k.r > 1 ? launch<T, ACC, 8, BACK, true>(a, k.r, s) : launch<T, ACC, 8, BACK, false>(a, 1, s);
-        case 32: return launch<T, ACC, 32, BACK, false>(a, 1, s);
-        default: return launch<T, ACC, 64, BACK, false>(a, 1, s);
+        case 4: return k.r > 1 ? launch<T, ACC, 4, BACK, true>(a, k.r, err, s) : launch<T, ACC, 4, BACK, false>(a, 1, err, s);
+        case 8: return k.r > 1 ? launch<T, ACC, 8, BACK, true>(a, k.r, err, s) : launch<T, ACC, 8, BACK, false>(a, 1, err, s);
+        case 32: return launch<T, ACC, 32, BACK, false>(a, 1, err, s);
+        default: return launch<T, ACC, 64, BACK, false>(a, 1, err, s);
     }
 }
 // elements that may be moved at once: every row of every tensor starts on that many, and holds a multiple of them
 template <bool BACK>
-cudaError_t run(int dt, const RecurArgs& a, cudaStream_t s) {
+cudaError_t run(int dt, const RecurArgs& a, int* err, cudaStream_t s) {
     const size_t z = dt ? 2 : 4;
     uint64_t m = (uint64_t)a.C * z | (uintptr_t)a.z | (uintptr_t)a.v | (uint64_t)(a.z_b | a.z_t | a.v_b | a.v_t) * z;
     if (BACK) m |= (uintptr_t)a.dy | (uintptr_t)a.dz | (uintptr_t)a.dv | (uint64_t)(a.dy_b | a.dy_t | a.dz_b | a.dz_t | a.dv_b | a.dv_t) * z;
     else m |= (uintptr_t)a.y | (uint64_t)(a.y_b | a.y_t) * z;
-    if (dt) return m % 16 == 0 ? pick<bf16, 8, BACK>(a, s) : m % 4 == 0 ? pick<bf16, 2, BACK>(a, s) : pick<bf16, 1, BACK>(a, s);
-    return m % 16 == 0 ? pick<float, 4, BACK>(a, s) : pick<float, 1, BACK>(a, s);
+    if (dt) return m % 16 == 0 ? pick<bf16, 8, BACK>(a, err, s) : m % 4 == 0 ? pick<bf16, 2, BACK>(a, err, s) : pick<bf16, 1, BACK>(a, err, s);
+    return m % 16 == 0 ? pick<float, 4, BACK>(a, err, s) : pick<float, 1, BACK>(a, err, s);
 }
 
 }  // namespace
@@ -721,20 +720,20 @@ size_t recur_saved_bytes(int, long B, long T, long C) {
     return (size_t)B * ((T + tile - 1) / tile) * C * sizeof(float);
 }
 
-cudaError_t recur_forward(int dt, const RecurArgs& a, cudaStream_t s) {
+cudaError_t recur_forward(int dt, const RecurArgs& a, int* err, cudaStream_t s) {
     if (a.B * a.C == 0) return cudaSuccess;
     Scope sc(KC_RECUR_FWD, 8.0 * a.B * a.T * a.C, 3.0 * a.B * a.T * a.C * (dt ? 2 : 4), s);
     if (a.T == 1 && !a.saved) {
         const unsigned blocks = (unsigned)((a.B * a.C + 127) / 128);
         return dt ? klaunch(recur_step_k<bf16>, blocks, 128, 0, s, a) : klaunch(recur_step_k<float>, blocks, 128, 0, s, a);
     }
-    return run<false>(dt, a, s);
+    return run<false>(dt, a, err, s);
 }
 
-cudaError_t recur_backward(int dt, const RecurArgs& a, cudaStream_t s) {
+cudaError_t recur_backward(int dt, const RecurArgs& a, int* err, cudaStream_t s) {
     if (a.B * a.C == 0) return cudaSuccess;
     Scope sc(KC_RECUR_BWD, 16.0 * a.B * a.T * a.C, 5.0 * a.B * a.T * a.C * (dt ? 2 : 4), s);
-    return run<true>(dt, a, s);
+    return run<true>(dt, a, err, s);
 }
 
 }  // namespace fdg

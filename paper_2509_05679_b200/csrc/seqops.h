@@ -33,12 +33,11 @@ struct RecurArgs {
     void *dz, *dv; long dz_b, dz_t, dv_b, dv_t;
     float* dstate;                           // gradient of h_0, or nullptr: not needed
     int accum;                               // dz, dv are added to
-    int* err;                                // device word that a kernel sets (from 0) when a wait of its gave up, or nullptr
-    long long wait_copies, wait_peers;       // cycles that waits last (filled in at the launch)
 };
 size_t recur_saved_bytes(int dt, long B, long T, long C);
-cudaError_t recur_forward(int dt, const RecurArgs& a, cudaStream_t s);
-cudaError_t recur_backward(int dt, const RecurArgs& a, cudaStream_t s);
+// err: device word that a kernel sets (from 0) when a wait of its gave up, or nullptr
+cudaError_t recur_forward(int dt, const RecurArgs& a, int* err, cudaStream_t s);
+cudaError_t recur_backward(int dt, const RecurArgs& a, int* err, cudaStream_t s);
 
 // ---- distillation loss (distill.cu): see fdg_distill_loss
 struct DistillArgs {
