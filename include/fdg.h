@@ -76,7 +76,9 @@ typedef enum {
                                   0..c_in-1 (padding) gives zeros.  flags & 1: times sqrt(c_out)            */
     FDG_RECURRENCE = 10        /* gated linear recurrence along a sample's positions (rows of the image one after the
                                   other) from a zero state, c_in = 2 c_out: channels 0..c_out-1 are the gates, the others
-                                  the values (see fdg_recurrence_forward)                                   */
+                                  the values (see fdg_recurrence_forward).  Every position counts: a sample has no
+                                  length here, so padding (ids outside the table) is gone through as rows of zeros and
+                                  counted by an average behind it, and no state is carried from step to step    */
 } fdg_layer_kind;
 
 /* flags: bit 0 = has bias (LINEAR / CONV*), "projection shortcut" (RES_ADD), or "scaled" (EMBEDDING).
@@ -200,7 +202,8 @@ FDG_API fdg_status fdg_set_params_worker(fdg_ctx* ctx, int32_t worker, const flo
 FDG_API fdg_status fdg_step(fdg_ctx* ctx, const void* dev_inputs, const int32_t* dev_labels,
                     float* host_loss_or_null);
 
-/* Train against a teacher as well: from now on the loss of a sample is that of fdg_distill_loss, with `top` of the teacher's logits per sample, and a sample
+/* (One row of logits per sample, as every network here ends in: a loss per token of a sequence is fdg_distill_loss's own call, in a caller's own loop.)
+ * Train against a teacher as well: from now on the loss of a sample is that of fdg_distill_loss, with `top` of the teacher's logits per sample, and a sample
  * whose label is outside 0..num_classes-1 does not count (its loss and gradient are zero; the means over M count it).  Call it before the first step
  * (FDG_ERR_STATE later, or a second time); num_classes <= 262144, 1 <= top <= 1024, temperature and weight as there.  The steps are then
  * fdg_step_distill's: fdg_step and fdg_step_host return FDG_ERR_STATE. */

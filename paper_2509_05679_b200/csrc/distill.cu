@@ -460,7 +460,8 @@ cudaError_t launch(const DistillArgs& a, cudaStream_t s) {
         return klaunch(distill_warp_k<TI, TO, SQ, HARD>, (unsigned)((a.M + WARPS - 1) / WARPS), THREADS, 0, s, a);
     // A CTA's share of a row: up to 100 KB, so that two fit on an SM (three up to 64 KB) and one copies while others compute; smaller where there are too few rows for
     // the SMs, down to 16 KB (8 rows of 32000 bf16 8.3 us, 10.4 in one share each).  1500 rows of 100003 fp32 logits: 271 us in four shares, 327 in eight (more time in the cluster's barriers), 295 in four with 512 threads
-    // a CTA (more time in the joins).
+    // a CTA (more time in the joins).  With eight CTAs a row at most, shares grow beyond that from 204800 fp32 logits on, to 131 KB and the entries at 262144: one CTA to an SM, and nothing
+    // copies while it computes (600 rows of 262144 fp32 455 us for 192 of bytes, 700 of 204800 302 for 175).
     constexpr int E = Chunk<TI>::E;
     const long chunks = (a.V + E - 1) / E + 1;      // with one more for a row that starts inside a chunk
     int R = 1;
@@ -478,6 +479,8 @@ cudaError_t launch(const DistillArgs& a, cudaStream_t s) {
         const long rows = std::min<long>(a.M, resident.ask((const void*)kernel, R, smem));       // at once
         return klaunch_cluster(kernel, (unsigned)(rows * R), THREADS, (size_t)smem, s, R, a, R, share);
     }
+    // Three CTAs an SM, whatever fits: shares over 64 KB, of which two do, leave the third's rows to a short wave of their own (bf16, bytes' time and time: 4096 rows of 32000 80 and 111 us,
+    // 3200 of 40000 78 and 150, 2600 of 50257 80 and 136; fp32 3200 of 20000 78 and 121).
     static OncePerDevice once;
     const auto kernel = distill_row_k<TI, TO, SQ, HARD, false>;
     const cudaError_t e = allow_smem(once, (const void*)kernel, most);

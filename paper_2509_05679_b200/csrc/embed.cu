@@ -110,7 +110,7 @@ __device__ __forceinline__ void fill_rows(Tokens token, int n, float* dtable, lo
 
 // ---- gradient of few tokens, in one launch
 // Sorted, 512 ids of 32000 x 1024 take 38 us instead of 26 (1000 x 128: 17 instead of 6), 2048 take 39 instead of 38; the more equal ones there are, the longer a warp adds: where three in
-// ten are one id, 512 take 60 (27), sorted 37 (17).
+// ten are one id, 512 take 60 (27), sorted 37 (17).  (Which ids there are is not known on the host; the line is for ids that mostly differ.)
 constexpr int FEW = 512;
 // CTAs 0 .. sum_ctas - 1: a warp per token and 32 N channels; it goes on if no earlier token is the same, and adds up all that are, in order.  The
 // others fill the rows that no token names.
@@ -322,7 +322,7 @@ struct Left {
     int2* chain;            // and these tiles and tokens, in any order
 };
 
-constexpr int BATCH = 8;                        // rows on their way at once
+constexpr int BATCH = 8;                        // rows on their way at once (with whole vectors 80 registers do not quite hold them: 20 and 28 bytes a thread, fp32 and bf16, are spilled)
 template <typename T, int N>
 __global__ void __launch_bounds__(256, 3) embed_sums_k(const uint2* __restrict__ list, const T* __restrict__ dy, long dys, int C, float scale, int accum,
                                                     float* __restrict__ dtable, Left left, Plan p) {
@@ -457,6 +457,8 @@ Plan plan(int dt, long n, long C, int vec) {
     const long threads = (C + most - 1) / most;                 // of a tile, with whole vectors
     // Tiles: the shortest whose teams the device holds at once (three CTAs an SM), or, where even the longest are more, 32: many short waves instead of a little more than one.
     // 16384 x 1024 bf16 in tiles of 16, 32, 64, 128: 55, 49, 51, 68 us; 131072 x 1024: 205, 191, 193, 218; 131072 x 256: 69, 63, 59, 67; a million x 64: 275, 259, 236, 216.
+    // At the border, 113664 x 1024 of 32000 rows, and behind it 32 is not the best: in tiles of 32, 64, 128 just under it 135, 128, 121 us (128 is taken), just over it 136, 126, 120 (32 is),
+    // 250000 245, 233, 230; 131072 of 131072 rows 205, 202, 215.
     const long room = 148l * 3 * 256;
     int t = 16;
     while (t < 128 && (n + t - 1) / t * threads > room) t *= 2;
