@@ -50,6 +50,10 @@ Scope::Scope(int cls_, double flops, double bytes, cudaStream_t s) : cls(cls_), 
         KernelStat& d = prof::g_detail[std::string(kClassNames[cls]) + "[" + detail + "]"];
         d.launches += 1; d.flops += flops; d.bytes += bytes;
     }
+    // a caller's capture (of an operator's call): the event would become a node of its graph and have no time
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) { cudaGetLastError(); return; }
+    if (cap != cudaStreamCaptureStatusNone) return;
     a = prof::get_event();
     cudaEventRecord(a, st);
 }
@@ -71,12 +75,12 @@ int profile_read(KernelStat* out, const char** names) {
     std::lock_guard<std::mutex> lk(prof::g_mu);
     for (auto& r : prof::g_drecs) {
         float ms = 0.f;
-        if (cudaEventElapsedTime(&ms, r.a, r.b) == cudaSuccess) prof::g_detail[r.key].ms += ms;
+        if (launched(cudaEventElapsedTime(&ms, r.a, r.b))) prof::g_detail[r.key].ms += ms;       // (no error is left for the next step to be blamed for)
     }
     prof::g_drecs.clear();
     for (auto& r : prof::g_recs) {
         float ms = 0.f;
-        if (cudaEventElapsedTime(&ms, r.a, r.b) == cudaSuccess) prof::g_stat[r.cls].ms += ms;
+        if (launched(cudaEventElapsedTime(&ms, r.a, r.b))) prof::g_stat[r.cls].ms += ms;
         prof::g_pool.push_back(r.a); prof::g_pool.push_back(r.b);
     }
     prof::g_recs.clear();

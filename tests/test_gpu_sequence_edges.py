@@ -91,3 +91,61 @@ def test_replicas_with_many_padded_ids(orc):
         for r in range(3):
             assert max_rel_err(ctx.params_worker(r), o.params(r), net.layers)[0] <= 1e-5, (t, r)
     ctx.close()
+
+
+def test_a_callers_streams_profiles_and_a_second_run():
+    """A distilling network on the caller's streams, under the profiler and after a second fdg_set_params: the same weights, and the operators' kernels in the profile."""
+    import torch
+    from paper_2509_05679_b200 import binding
+    layers = [(sy.EMBEDDING, 60, 32, 1, 1), (sy.CONV1X1, 32, 64, 1, 1), (sy.RECURRENCE, 64, 32, 1, 0), (sy.CONV1X1, 32, 32, 1, 1), (sy.RECURRENCE, 32, 16, 1, 0)] + TAIL
+    net = sy.Net("tokens", layers, [3], 1, 40, 1, 10, 2, 8, 0.1, "bf16")
+    p0 = sy.round_to_bf16(sy.init_params(net.layers, 0))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    out = []
+    for kw, profile in ((dict(), False), (dict(streams=[s.cuda_stream for s in streams]), False), (dict(), True)):
+        ctx = make_ctx(net, p0, grid_sms=148, **kw)
+        ctx.set_distill(4, 2.0, 0.5)
+        for _ in range(2):
+            ctx.set_params(p0)
+            ctx.profile(profile)
+            for t in range(9):
+                held = [binding.to_device("bf16", sy.batch_inputs(net, t))] + [torch.from_numpy(a).cuda() for a in (sy.batch_labels(net, t), *sy.batch_teacher(net, t, 4))]
+                torch.cuda.synchronize()
+                ctx.step_distill(*held)
+                ctx.wait_ingest()
+            out.append(ctx.params())
+        if profile:
+            seen = {name for name, r in ctx.profile_read().items() if r["launches"] > 0}
+            ctx.profile(False)
+            assert {"embed_fwd", "embed_grad", "recur_fwd", "recur_bwd", "distill"} <= seen
+        ctx.close()
+    assert np.isfinite(out[0]).all() and not np.array_equal(out[0], p0)
+    assert all(np.array_equal(out[0], o) for o in out[1:])
+
+
+def test_operators_captured_under_the_profiler(orc):
+    """A caller's graph of operators recorded while a context's profiler is on: its launches are counted, have no time, and no step is blamed for them; calls outside of it are timed."""
+    import torch
+    from paper_2509_05679_b200 import binding, operators as ops
+    net = sy.Net("mlp", [(sy.LINEAR, 8, 16, 1, 1), (sy.LINEAR, 16, 10, 1, 1)], [], 1, 1, 8, 10, 2, 8, 0.1, "fp32")
+    ctx = make_ctx(net, sy.init_params(net.layers, 0))
+    x, y = binding.to_device("fp32", sy.batch_inputs(net, 0)), torch.from_numpy(sy.batch_labels(net, 0)).cuda()
+    tok = torch.zeros(700, dtype=torch.int32, device="cuda")
+    dy = torch.ones(700, 32, device="cuda")
+    run = lambda: (ops.embedding_grad(tok, dy, 50), ops.recurrence(dy.view(7, 100, 32), dy.view(7, 100, 32)))
+    run()
+    ctx.profile(True)
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    graph.replay()
+    want = run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1][0], want[1][0])
+    seen = ctx.profile_read()
+    ctx.profile(False)
+    ctx.step(x, y)
+    assert ctx.step(x, y, want_loss=True) > 0
+    for name in ("embed_grad", "recur_fwd"):
+        assert seen[name]["launches"] == 3 and seen[name]["ms"] > 0
+    ctx.close()
